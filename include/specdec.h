@@ -54,7 +54,7 @@
 extern "C" {
 #endif
 
-#define SPECDEC_ABI_VERSION 5
+#define SPECDEC_ABI_VERSION 6
 
 typedef enum {
   SPECDEC_OK = 0,
@@ -75,6 +75,7 @@ typedef enum { SPECDEC_F32 = 0, SPECDEC_BF16 = 1, SPECDEC_F16 = 2 } specdec_dtyp
                                         fit the batch width, the pool or its token row */
 #define SPECDEC_DEV_SLOT_LEN 0x20u   /* write-back: lens[slot] != Lb - pads[i] on entry */
 #define SPECDEC_DEV_BAD_UNIFORM 0x40u /* a uniform outside [0, 1) (clamped into it)       */
+#define SPECDEC_DEV_EMPTY_MASK 0x80u  /* a grammar mask that allows no token of its row    */
 
 /* Limits checked by the host. */
 #define SPECDEC_MAX_B 65536
@@ -83,6 +84,8 @@ typedef enum { SPECDEC_F32 = 0, SPECDEC_BF16 = 1, SPECDEC_F16 = 2 } specdec_dtyp
 #define SPECDEC_MAX_WIDTH 16777216    /* W_in, cap and pm_cap                      */
 #define SPECDEC_MAX_D 4096
 #define SPECDEC_MAX_SAMPLE_V 8388608  /* vocabulary of stochastic verification          */
+#define SPECDEC_MAX_HEAD_D 256        /* head size of the append and attention calls       */
+#define SPECDEC_MAX_BIAS 1024         /* biases of a sequence in specdec_process_logits    */
 #define SPECDEC_NOALLOC_SCRATCH_BYTES 4194304  /* library scratch of specdec_step_noalloc */
 
 /* A bf16 KV cache [L][2][B][H][cap][D], contiguous, D fastest.  One
@@ -568,6 +571,146 @@ specdec_status_t specdec_varlen_rollback(const specdec_varlen_t* src, const spec
                                          const int32_t* cu_in, const int32_t* n_acc, int32_t B,
                                          int32_t k, int32_t max_len, int32_t* cu_out, int64_t* pos,
                                          int64_t pos_cap, uint32_t* dev_status, void* stream);
+
+/* ---- around the forward: append, attention, logits ---------------------------
+ *
+ * A verify forward runs T = k+1 tokens of every sequence (a draft or plain
+ * decode step T = 1) through each layer: their queries, keys and values are
+ * normed and rotated, the keys and values appended to the cache, and the
+ * queries attend over the cached entries and the window.  The calls below do
+ * this for one layer, on either of two layouts:
+ *
+ *   _window  the left-padded batch of specdec_step: kv [L][2][B][H][cap][D],
+ *            row i holds c_i = W_in - T - pad_in[i] cached entries from column
+ *            pad_in[i] on, the window in columns [W_in - T, W_in).
+ *   _paged   pages of a pool cache [L][2][N][H][P][D] (pool->B = N pages of
+ *            pool->cap = P entries, any P >= 1): entry j of sequence i lies in
+ *            page table[i][j / P] at column j % P; c_i = lens[i] entries are
+ *            cached, the window's are entries lens[i] .. lens[i] + T - 1.
+ *            EXSpec's pool of whole sequences is the case of one page each
+ *            (table = slots, a stride of 1), so that a forward needs no
+ *            gather.  After verification lens[i] grows by n_acc[i] + 1:
+ *            rejected entries are overwritten by the next window.
+ *
+ * The head size D is a multiple of 8, at most SPECDEC_MAX_HEAD_D.  Hq query
+ * heads share the cache's H heads: Hq is a multiple of H, query head h reads
+ * cache head h / (Hq / H).  1 <= T <= SPECDEC_MAX_K + 1, B*T <=
+ * SPECDEC_MAX_ROWS.  Entries outside a sequence's own (padding, columns past
+ * the window, the rest of a page) are never read, whatever they hold, and a
+ * query reads no value of the entries after its own.
+ *
+ * A sequence whose padding is outside [0, W_in - T] is left untouched and
+ * flagged SPECDEC_DEV_BAD_PAD_IN; one whose length is negative or too long
+ * (for the table in an append, for max_len in an attention) or one of whose
+ * pages is outside [0, N) is left untouched and flagged SPECDEC_DEV_BAD_SLOT.
+ * Table places that no entry needs are not read as pages and may hold
+ * anything.  Sequences must not share the pages that a call appends to (not
+ * checked: the contents of the shared entries are then unspecified); shared
+ * pages are read by attention like any others.
+ */
+
+/*
+ * Norm, rotation and append.  For every token of the window, head by head:
+ *   x = x / sqrt(mean(x^2) + eps) * weight     queries and keys, where the
+ *                                              weight is given
+ *   (a, b) = (a cos t - b sin t, b cos t + a sin t),  t = position *
+ *                                              inv_freq[j], queries and keys
+ * for the pairs (x[j], x[j + n_freq]), or (x[2j], x[2j+1]) with `adjacent`,
+ * j < n_freq; elements beyond 2 * n_freq are not rotated.  The position of
+ * window slot r is c_i + r (invariant I2: the entries before it).  Then the
+ * keys and values go to the cache's layer `layer`, the queries to q_out.
+ *
+ *   qkv       [B][T][Hq + 2H][D] of `dtype` (SPECDEC_F32 / _BF16 / _F16): the
+ *             projections' output, queries, then keys, then values; contiguous,
+ *             16-byte aligned.
+ *   q_norm, k_norm  [D] of `dtype`, or NULL (no norm).  eps >= 0, finite.
+ *   inv_freq  float [n_freq], 0 <= n_freq <= D/2 (NULL when 0); the angle is
+ *             formed in fp64 from these values.
+ *   q_out     bf16 [B][T][Hq][D] out, 16-byte aligned.
+ * The arithmetic is fp32 with one rounding to bf16 at the end.
+ */
+specdec_status_t specdec_append_window(const void* qkv, int32_t dtype, int32_t T, int32_t Hq, const void* q_norm,
+                                       const void* k_norm, float eps, const float* inv_freq, int32_t n_freq,
+                                       int32_t adjacent, const specdec_kv_t* kv, int32_t layer, int32_t W_in,
+                                       const int32_t* pad_in, void* q_out, uint32_t* dev_status, void* stream);
+
+/* table int32 [B][table_stride], lens int32 [B]; lens[i] + T <= table_stride * P. */
+specdec_status_t specdec_append_paged(const void* qkv, int32_t dtype, int32_t B, int32_t T, int32_t Hq,
+                                      const void* q_norm, const void* k_norm, float eps, const float* inv_freq,
+                                      int32_t n_freq, int32_t adjacent, const specdec_kv_t* pool, int32_t layer,
+                                      const int32_t* table, int64_t table_stride, const int32_t* lens, void* q_out,
+                                      uint32_t* dev_status, void* stream);
+
+/*
+ * Attention of the window.  Query r of sequence i attends over entries
+ * 0 .. c_i + r (the cached ones, and the window up to itself):
+ *   out[i][r][h] = sum_j p_j v_j,  p = softmax_j(scale * q[i][r][h] . k_j)
+ *
+ *   q         bf16 [B][T][Hq][D], 16-byte aligned (specdec_append_*'s q_out).
+ *   scale     finite (1 / sqrt(D) in most models).
+ *   out       bf16 [B][T][Hq][D] out, 16-byte aligned.
+ *   workspace specdec_attend_workspace_bytes(B, T, Hq, H, D, max_len) bytes,
+ *             16-byte aligned, with max_len = W_in for the batch; it needs no
+ *             initialisation.
+ * Scores, the softmax's statistics and the sums are fp32; the weights p are
+ * rounded to bf16 for the matrix cores, and their sum is taken of the rounded
+ * ones.  The result does not depend on the order in which workgroups run.
+ */
+size_t specdec_attend_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t H, int32_t D, int32_t max_len);
+
+specdec_status_t specdec_attend_window(const void* q, int32_t T, int32_t Hq, float scale, const specdec_kv_t* kv,
+                                       int32_t layer, int32_t W_in, const int32_t* pad_in, void* out, void* workspace,
+                                       size_t workspace_bytes, uint32_t* dev_status, void* stream);
+
+/* max_len: host bound on lens[i] + T, T <= max_len <= table_stride * P. */
+specdec_status_t specdec_attend_paged(const void* q, int32_t B, int32_t T, int32_t Hq, float scale,
+                                      const specdec_kv_t* pool, int32_t layer, const int32_t* table,
+                                      int64_t table_stride, const int32_t* lens, int32_t max_len, void* out,
+                                      void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream);
+
+/*
+ * Penalties for repeated tokens, biases and a grammar mask on the logits of a
+ * window, ahead of specdec_verify_greedy / specdec_verify_sample (k = 0: the
+ * logits of a draft or plain decode step).  For logit x of token v in slot r
+ * of sequence i, in this order:
+ *   x = x > 0 ? x / repetition[i] : x * repetition[i]   where v occurs in the
+ *                        slot's history;
+ *   x = x - (frequency[i] * n + presence[i])            where n, the times that
+ *                        v occurs in the history past its prompt, is above 0;
+ *   x = x + bias         for each of the sequence's biases on v, in their order;
+ *   x = -inf             where bit v % 32 of mask[i][r][v / 32] is clear.
+ * The history of slot r is s[i][begin[i] .. end_i] (the sequence's tokens and
+ * the pending one in column end_i) and then draft[i][0 .. r); its prompt is
+ * the first prompt[i] of these.  Tokens and bias ids outside [0, V) count for
+ * nothing.
+ *
+ *   logits, out  [B][k+1][V] of `dtype`, contiguous, aligned to the element
+ *             size; out == logits: in place; otherwise they must not overlap.
+ *   s         int32 [B][s_stride]: token rows; in the left-padded batch begin =
+ *             pad_in and end_i = width = W_in - (k+1) for every row (lens
+ *             NULL); in a pool of unpadded rows begin is NULL (0) and end_i =
+ *             lens[i].  0 <= width < s_stride.  s and draft may be NULL when
+ *             none of the three penalties is given.
+ *   draft     int32 [B][k].
+ *   begin, lens, prompt           int32 [B], each may be NULL (0, width, 0).
+ *   repetition, presence, frequency  float [B], each may be NULL (no such
+ *             penalty).
+ *   bias_ids, bias  int32 / float [B][n_bias], n_bias <= SPECDEC_MAX_BIAS.
+ *   mask      uint32 [B][k+1][mask_stride], mask_stride >= ceil(V / 32), or
+ *             NULL.
+ * A sequence without 0 <= begin[i] <= end_i < s_stride is left untouched and
+ * flagged SPECDEC_DEV_BAD_PAD_IN.  A slot whose mask allows no token becomes
+ * -inf throughout and is flagged SPECDEC_DEV_EMPTY_MASK: greedy verification
+ * then answers token 0, stochastic verification an unspecified one.
+ * The arithmetic is fp32 with one rounding to `dtype` at the end.
+ * Limits as specdec_verify_greedy.
+ */
+specdec_status_t specdec_process_logits(const void* logits, void* out, int32_t dtype, int32_t B, int32_t k, int32_t V,
+                                        const int32_t* s, int64_t s_stride, int32_t width, const int32_t* draft,
+                                        const int32_t* begin, const int32_t* lens, const int32_t* prompt,
+                                        const float* repetition, const float* presence, const float* frequency,
+                                        const int32_t* bias_ids, const float* bias, int32_t n_bias,
+                                        const uint32_t* mask, int64_t mask_stride, uint32_t* dev_status, void* stream);
 
 /*
  * Kernel timers (for measurement; off by default).  specdec_timing_enable

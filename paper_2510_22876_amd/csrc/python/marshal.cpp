@@ -13,6 +13,7 @@
 #include <ATen/core/Tensor.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <initializer_list>
 
 #include "specdec.h"
@@ -31,6 +32,12 @@ struct Library {
   decltype(&specdec_gather_batch) gather_batch;
   decltype(&specdec_scatter_accepted) scatter_accepted;
   decltype(&specdec_varlen_rollback) varlen_rollback;
+  decltype(&specdec_append_window) append_window;
+  decltype(&specdec_append_paged) append_paged;
+  decltype(&specdec_attend_workspace_bytes) attend_workspace_bytes;
+  decltype(&specdec_attend_window) attend_window;
+  decltype(&specdec_attend_paged) attend_paged;
+  decltype(&specdec_process_logits) process_logits;
 } lib;
 PyObject* get_device = nullptr;   // torch's current device, and the current stream of a device as an integer
 PyObject* get_stream = nullptr;
@@ -152,6 +159,14 @@ void* stream_of(PyObject* o) {
     throw Leave{};
   }
   return s;
+}
+
+// The kernels run on the current device.
+void on_current_device(const at::Tensor& t) {
+  PyObject* dev = PyObject_CallNoArgs(get_device);
+  const long d = dev ? PyLong_AsLong(dev) : -1;
+  Py_XDECREF(dev);
+  need(d >= 0 && t.is_cuda() && t.get_device() == d);
 }
 
 // Runs the library call without the interpreter lock, as ctypes does.
@@ -391,6 +406,175 @@ PyObject* varlen_rollback(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// The arguments that both appends share.
+struct Append {
+  const void *qkv, *q_norm, *k_norm;
+  const float* inv_freq = nullptr;
+  int32_t dtype, B, T, Hq, n_freq = 0, adjacent;
+  float eps;
+  specdec_kv_t kv;
+  void* q_out;
+  Append(PyObject* qkv_, PyObject* kv_, PyObject* q_out_, PyObject* const* a) {   // a: inv_freq, q_norm, k_norm, eps, adjacent
+    const at::Tensor& t = tensor(qkv_);
+    const at::ScalarType type = t.scalar_type();
+    dtype = type == at::kFloat ? SPECDEC_F32 : type == at::kBFloat16 ? SPECDEC_BF16 : SPECDEC_F16;
+    need((dtype != SPECDEC_F16 || type == at::kHalf) && t.dim() == 4 && t.is_cuda() && t.is_contiguous());
+    for (int d : {0, 1, 2, 3}) need(t.size(d) <= INT32_MAX);
+    on_current_device(t);
+    kv = cache(kv_);
+    B = static_cast<int32_t>(t.size(0));
+    T = static_cast<int32_t>(t.size(1));
+    const int64_t q_heads = t.size(2) - 2 * static_cast<int64_t>(kv.H);
+    need(t.size(3) == kv.D && q_heads >= 1);
+    Hq = static_cast<int32_t>(q_heads);
+    qkv = pointer(t);
+    q_out = dense<void>(q_out_, at::kBFloat16, {B, T, Hq, kv.D});
+    if (a[0] != Py_None) {
+      const int64_t n = tensor(a[0]).numel();
+      need(n <= INT32_MAX);
+      n_freq = static_cast<int32_t>(n);
+      inv_freq = dense<float>(a[0], at::kFloat, {n});
+    }
+    q_norm = dense_or_none<void>(a[1], type, {kv.D});
+    k_norm = dense_or_none<void>(a[2], type, {kv.D});
+    need(PyFloat_CheckExact(a[3]) && PyBool_Check(a[4]));
+    eps = static_cast<float>(PyFloat_AS_DOUBLE(a[3]));
+    adjacent = a[4] == Py_True;
+  }
+};
+
+// (qkv, kv, layer, W_in, pad_in, q_out, inv_freq, q_norm, k_norm, eps,
+//  adjacent, dev_status, stream)
+PyObject* append_window(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 13, [&] {
+    const Append p(a[0], a[1], a[5], a + 6);
+    need(p.kv.B == p.B);
+    const int32_t layer = integer(a[2]), W_in = integer(a[3]), *pad_in = ints(a[4], {p.B});
+    uint32_t* dev = status(a[11]);
+    void* st = stream_of(a[12]);
+    return PyLong_FromLong(unlocked([&] {
+      return lib.append_window(p.qkv, p.dtype, p.T, p.Hq, p.q_norm, p.k_norm, p.eps, p.inv_freq, p.n_freq, p.adjacent, &p.kv,
+                               layer, W_in, pad_in, p.q_out, dev, st);
+    }));
+  });
+}
+
+// (qkv, pool, layer, table, lens, q_out, inv_freq, q_norm, k_norm, eps,
+//  adjacent, dev_status, stream)
+PyObject* append_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 13, [&] {
+    const Append p(a[0], a[1], a[5], a + 6);
+    int64_t table_stride = 0;
+    const int32_t layer = integer(a[2]), *table = rows<int32_t>(a[3], at::kInt, p.B, &table_stride), *lens = ints(a[4], {p.B});
+    uint32_t* dev = status(a[11]);
+    void* st = stream_of(a[12]);
+    return PyLong_FromLong(unlocked([&] {
+      return lib.append_paged(p.qkv, p.dtype, p.B, p.T, p.Hq, p.q_norm, p.k_norm, p.eps, p.inv_freq, p.n_freq, p.adjacent,
+                              &p.kv, layer, table, table_stride, lens, p.q_out, dev, st);
+    }));
+  });
+}
+
+// The arguments that both attentions share.
+struct Attend {
+  const void* q;
+  int32_t B, T, Hq;
+  float scale;
+  specdec_kv_t kv;
+  void* out;
+  Workspace ws;
+  Attend(PyObject* q_, PyObject* kv_, PyObject* out_, PyObject* ws_, PyObject* scale_, int32_t max_len) {
+    const at::Tensor& t = tensor(q_);
+    need(t.dim() == 4);
+    for (int d : {0, 1, 2, 3}) need(t.size(d) <= INT32_MAX);
+    on_current_device(t);
+    kv = cache(kv_);
+    need(t.size(3) == kv.D);
+    B = static_cast<int32_t>(t.size(0));
+    T = static_cast<int32_t>(t.size(1));
+    Hq = static_cast<int32_t>(t.size(2));
+    q = dense<void>(q_, at::kBFloat16, {B, T, Hq, kv.D});
+    out = dense<void>(out_, at::kBFloat16, {B, T, Hq, kv.D});
+    ws = workspace(ws_, lib.attend_workspace_bytes(B, T, Hq, kv.H, kv.D, max_len));
+    if (scale_ == Py_None) {
+      scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(kv.D)));
+    } else {
+      need(PyFloat_CheckExact(scale_));
+      scale = static_cast<float>(PyFloat_AS_DOUBLE(scale_));
+    }
+  }
+};
+
+// (q, kv, layer, W_in, pad_in, out, workspace, scale, dev_status, stream)
+PyObject* attend_window(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&] {
+    const int32_t layer = integer(a[2]), W_in = integer(a[3]);
+    const Attend p(a[0], a[1], a[5], a[6], a[7], W_in);
+    need(p.kv.B == p.B);
+    const int32_t* pad_in = ints(a[4], {p.B});
+    uint32_t* dev = status(a[8]);
+    void* st = stream_of(a[9]);
+    return PyLong_FromLong(unlocked([&] {
+      return lib.attend_window(p.q, p.T, p.Hq, p.scale, &p.kv, layer, W_in, pad_in, p.out, p.ws.data, p.ws.bytes, dev, st);
+    }));
+  });
+}
+
+// (q, pool, layer, table, lens, max_len, out, workspace, scale, dev_status, stream)
+PyObject* attend_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 11, [&] {
+    const int32_t layer = integer(a[2]), max_len = integer(a[5]);
+    const Attend p(a[0], a[1], a[6], a[7], a[8], max_len);
+    int64_t table_stride = 0;
+    const int32_t *table = rows<int32_t>(a[3], at::kInt, p.B, &table_stride), *lens = ints(a[4], {p.B});
+    uint32_t* dev = status(a[9]);
+    void* st = stream_of(a[10]);
+    return PyLong_FromLong(unlocked([&] {
+      return lib.attend_paged(p.q, p.B, p.T, p.Hq, p.scale, &p.kv, layer, table, table_stride, lens, max_len, p.out,
+                              p.ws.data, p.ws.bytes, dev, st);
+    }));
+  });
+}
+
+// (logits, out, s, width, draft, begin, lens, prompt, repetition, presence,
+//  frequency, bias_ids, bias, mask, dev_status, stream)
+PyObject* process_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 16, [&] {
+    const Logits l = logits_of(a[0]);
+    const int64_t B = l.B;
+    on_current_device(tensor(a[0]));
+    void* out = dense<void>(a[1], l.type, {B, l.k + 1, l.V});
+    int64_t s_stride = 0, n_bias = 0, words = 0;
+    const int32_t* s = a[2] != Py_None ? rows<int32_t>(a[2], at::kInt, B, &s_stride) : nullptr;
+    const int32_t width = integer(a[3]), *draft = ints_or_none(a[4], {B, l.k});
+    const int32_t *begin = ints_or_none(a[5], {B}), *lens = ints_or_none(a[6], {B}), *prompt = ints_or_none(a[7], {B});
+    const float* penalty[3];
+    for (int j = 0; j < 3; ++j) penalty[j] = dense_or_none<float>(a[8 + j], at::kFloat, {B});
+    need((a[11] == Py_None) == (a[12] == Py_None));
+    const int32_t* bias_ids = nullptr;
+    const float* bias = nullptr;
+    if (a[11] != Py_None) {
+      bias_ids = rows<int32_t>(a[11], at::kInt, B, &n_bias);
+      bias = dense<float>(a[12], at::kFloat, {B, n_bias});
+      need(n_bias <= INT32_MAX);
+    }
+    const uint32_t* mask = nullptr;
+    if (a[13] != Py_None) {
+      const at::Tensor& m = tensor(a[13]);
+      need(m.dim() == 3);
+      words = m.size(2);
+      mask = dense<uint32_t>(a[13], at::kInt, {B, l.k + 1, words});
+    }
+    uint32_t* dev = status(a[14]);
+    void* st = stream_of(a[15]);
+    return PyLong_FromLong(unlocked([&] {
+      return lib.process_logits(l.data, out, l.dtype, l.B, l.k, l.V, s, s_stride, width, draft, begin, lens, prompt,
+                                penalty[0], penalty[1], penalty[2], bias_ids, bias, static_cast<int32_t>(n_bias), mask,
+                                words, dev, st);
+    }));
+  });
+}
+
 // connect(current device, raw stream of a device, {name: address of a library function})
 PyObject* connect(PyObject*, PyObject* args) {
   PyObject *dev, *st, *at;
@@ -402,7 +586,8 @@ PyObject* connect(PyObject*, PyObject* args) {
 #define SPECDEC_FN(f) {"specdec_" #f, reinterpret_cast<void**>(&lib.f)}
       SPECDEC_FN(workspace_bytes), SPECDEC_FN(sample_workspace_bytes), SPECDEC_FN(verify_greedy), SPECDEC_FN(verify_sample),
       SPECDEC_FN(step), SPECDEC_FN(step_noalloc), SPECDEC_FN(step_sample), SPECDEC_FN(gather_batch),
-      SPECDEC_FN(scatter_accepted), SPECDEC_FN(varlen_rollback)
+      SPECDEC_FN(scatter_accepted), SPECDEC_FN(varlen_rollback), SPECDEC_FN(append_window), SPECDEC_FN(append_paged),
+      SPECDEC_FN(attend_workspace_bytes), SPECDEC_FN(attend_window), SPECDEC_FN(attend_paged), SPECDEC_FN(process_logits)
 #undef SPECDEC_FN
   };
   for (const auto& f : table) {
@@ -431,6 +616,11 @@ PyMethodDef methods[] = {{"connect", connect, METH_VARARGS, nullptr},
                          FAST(gather_batch),
                          FAST(scatter_accepted),
                          FAST(varlen_rollback),
+                         FAST(append_window),
+                         FAST(append_paged),
+                         FAST(attend_window),
+                         FAST(attend_paged),
+                         FAST(process_logits),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Native argument marshalling of specdec.py.", -1, methods};
 

@@ -1157,6 +1157,228 @@ specdec_status_t specdec_varlen_rollback(const specdec_varlen_t* src, const spec
   return ok();
 }
 
+// ---- around the forward: append, attention, logits ---------------------------
+
+namespace {
+
+// The cache side of a window call: the layer's slabs as the kernels see them.
+specdec_status_t check_window(const specdec_kv_t* kv, const char* name, int32_t layer, int32_t B, int32_t T, int32_t Hq,
+                              specdec::CacheView* c) {
+  const specdec_status_t s = check_kv(kv, name);
+  if (s) return s;
+  if (B < 0 || B > SPECDEC_MAX_B) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "B=%d outside [0,%d]", B, SPECDEC_MAX_B);
+  if (T < 1 || T > SPECDEC_MAX_K + 1) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "T=%d outside [1,%d]", T, SPECDEC_MAX_K + 1);
+  if (static_cast<int64_t>(B) * T > SPECDEC_MAX_ROWS)
+    return fail(SPECDEC_ERR_INVALID_ARGUMENT, "B*T=%lld exceeds %d", (long long)B * T, SPECDEC_MAX_ROWS);
+  if (kv->D > SPECDEC_MAX_HEAD_D)
+    return fail(SPECDEC_ERR_UNSUPPORTED, "%s D=%d: heads of at most %d", name, kv->D, SPECDEC_MAX_HEAD_D);
+  if (layer < 0 || layer >= kv->L) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "layer=%d outside [0,%d)", layer, kv->L);
+  if (kv->H < 1 || Hq < 1 || Hq > SPECDEC_MAX_ROWS || Hq % kv->H != 0)
+    return fail(SPECDEC_ERR_INVALID_ARGUMENT, "Hq=%d is not a positive multiple of H=%d", Hq, kv->H);
+  if (B > 0 && (kv->B < 1 || kv->cap < 1)) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "%s is empty", name);
+  c->rows = kv->B;
+  c->H = kv->H;
+  c->D = kv->D;
+  c->cap = kv->cap;
+  c->row_stride = kv->cap * kv->D * kv->H;
+  const int64_t slab = c->row_stride * kv->B * 2;
+  c->k = static_cast<char*>(kv->data) + 2 * layer * slab;
+  c->v = static_cast<char*>(c->k) + slab;
+  return SPECDEC_OK;
+}
+
+specdec_status_t check_batch(const specdec_kv_t* kv, int32_t T, int32_t W_in, const int32_t* pad_in,
+                             specdec::CacheView* c) {
+  if (W_in < T || W_in > SPECDEC_MAX_WIDTH)
+    return fail(SPECDEC_ERR_INVALID_ARGUMENT, "W_in=%d outside [T=%d, %d]", W_in, T, SPECDEC_MAX_WIDTH);
+  c->width = W_in;
+  c->lens = pad_in;
+  if (kv->B == 0) return SPECDEC_OK;
+  if (kv->cap < W_in) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "kv cap=%lld < W_in=%d", (long long)kv->cap, W_in);
+  if (!pad_in) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "NULL pad_in");
+  if (!aligned(pad_in, 4)) return fail(SPECDEC_ERR_UNSUPPORTED, "int32 tensor not 4-byte aligned");
+  return SPECDEC_OK;
+}
+
+// `max_len` 0: the most that the table holds.
+specdec_status_t check_pages(const specdec_kv_t* pool, int32_t B, int32_t T, const int32_t* table, int64_t table_stride,
+                             const int32_t* lens, int32_t max_len, specdec::CacheView* c) {
+  if (table_stride < 1 || table_stride > SPECDEC_MAX_WIDTH)
+    return fail(SPECDEC_ERR_INVALID_ARGUMENT, "table_stride=%lld outside [1,%d]", (long long)table_stride, SPECDEC_MAX_WIDTH);
+  const int64_t held = table_stride * pool->cap;
+  if (max_len == 0) max_len = held < SPECDEC_MAX_WIDTH ? static_cast<int32_t>(held) : SPECDEC_MAX_WIDTH;
+  c->width = max_len;
+  c->table = table;
+  c->table_stride = table_stride;
+  c->lens = lens;
+  if (B == 0) return SPECDEC_OK;
+  if (max_len < T || max_len > held || max_len > SPECDEC_MAX_WIDTH)
+    return fail(SPECDEC_ERR_INVALID_ARGUMENT, "bound on entries %d outside [T=%d, table_stride*P=%lld]", max_len, T,
+                (long long)held);
+  if (!table || !lens) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "NULL table / lens");
+  if (!aligned(table, 4) || !aligned(lens, 4)) return fail(SPECDEC_ERR_UNSUPPORTED, "int32 tensor not 4-byte aligned");
+  return SPECDEC_OK;
+}
+
+// The index tensors of a call's cache: paddings, or lengths and table.
+Region lens_region(const specdec::CacheView& c, int32_t B) { return {c.lens, 4 * static_cast<int64_t>(B), c.table ? "lens" : "pad_in"}; }
+Region table_region(const specdec::CacheView& c, int32_t B) {
+  return {c.table, c.table ? 4 * static_cast<int64_t>(B) * c.table_stride : 0, "table"};
+}
+
+specdec_status_t append(const void* qkv, int32_t dtype, int32_t B, int32_t T, int32_t Hq, const void* q_norm,
+                        const void* k_norm, float eps, const float* inv_freq, int32_t n_freq, int32_t adjacent,
+                        const specdec_kv_t* kv, const specdec::CacheView& c, void* q_out, uint32_t* dev_status,
+                        void* stream) {
+  const int eb = logit_bytes(dtype);
+  if (eb == 0) return fail(SPECDEC_ERR_UNSUPPORTED, "qkv dtype %d not supported", dtype);
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "eps must be finite and >= 0");
+  if (n_freq < 0 || 2 * static_cast<int64_t>(n_freq) > c.D)
+    return fail(SPECDEC_ERR_INVALID_ARGUMENT, "n_freq=%d outside [0, D/2=%d]", n_freq, c.D / 2);
+  if (adjacent != 0 && adjacent != 1) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "adjacent=%d is neither 0 nor 1", adjacent);
+  if (B == 0) return ok();
+  if (!qkv || !q_out || (n_freq > 0 && !inv_freq)) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "NULL qkv / q_out / inv_freq");
+  if (!aligned(qkv, 16) || !aligned(q_out, 16)) return fail(SPECDEC_ERR_UNSUPPORTED, "qkv / q_out not 16-byte aligned");
+  if ((q_norm && !aligned(q_norm, eb)) || (k_norm && !aligned(k_norm, eb)))
+    return fail(SPECDEC_ERR_UNSUPPORTED, "norm weights not aligned to %d bytes", eb);
+  if ((inv_freq && !aligned(inv_freq, 4)) || (dev_status && !aligned(dev_status, 4)))
+    return fail(SPECDEC_ERR_UNSUPPORTED, "inv_freq / dev_status not 4-byte aligned");
+  const int64_t tokens = static_cast<int64_t>(B) * T, heads = static_cast<int64_t>(Hq) + 2 * c.H;
+  const specdec_status_t s = check_disjoint(
+      {{qkv, tokens * heads * c.D * eb, "qkv"}, {q_norm, static_cast<int64_t>(c.D) * eb, "q_norm"},
+       {k_norm, static_cast<int64_t>(c.D) * eb, "k_norm"}, {inv_freq, 4 * static_cast<int64_t>(n_freq), "inv_freq"},
+       lens_region(c, B), table_region(c, B)},
+      {{kv->data, kv_bytes(kv), "cache"}, {q_out, tokens * Hq * c.D * 2, "q_out"}, {dev_status, 4, "dev_status"}});
+  if (s) return s;
+  const specdec::AppendLaunch p{qkv, dtype, B, T, Hq, q_norm, k_norm, eps, inv_freq, n_freq, adjacent != 0, c, q_out, dev_status};
+  const hipError_t e = specdec::launch_append(p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "append launch");
+  return ok();
+}
+
+specdec_status_t attend(const void* q, int32_t B, int32_t T, int32_t Hq, float scale, const specdec_kv_t* kv,
+                        const specdec::CacheView& c, void* out, void* workspace, size_t workspace_bytes,
+                        uint32_t* dev_status, void* stream) {
+  if (!std::isfinite(scale)) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "scale must be finite");
+  if (B == 0) return ok();
+  if (!q || !out) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "NULL q / out");
+  if (!aligned(q, 16) || !aligned(out, 16)) return fail(SPECDEC_ERR_UNSUPPORTED, "q / out not 16-byte aligned");
+  if (dev_status && !aligned(dev_status, 4)) return fail(SPECDEC_ERR_UNSUPPORTED, "dev_status not 4-byte aligned");
+  const int64_t bytes = static_cast<int64_t>(B) * T * Hq * c.D * 2;
+  const specdec_status_t s = check_disjoint(
+      {{q, bytes, "q"}, {kv->data, kv_bytes(kv), "cache"}, lens_region(c, B), table_region(c, B)},
+      {{out, bytes, "out"}, {workspace, clamp_bytes(workspace_bytes), "workspace"}, {dev_status, 4, "dev_status"}});
+  if (s) return s;
+  const size_t need = specdec_attend_workspace_bytes(B, T, Hq, c.H, c.D, c.width);
+  if (!workspace) return fail(SPECDEC_ERR_WORKSPACE, "workspace is NULL (need %zu bytes)", need);
+  if (!aligned(workspace, 16)) return fail(SPECDEC_ERR_WORKSPACE, "workspace not 16-byte aligned");
+  if (workspace_bytes < need)
+    return fail(SPECDEC_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
+  const specdec::AttendLaunch p{q, B, T, Hq, scale, c, out, workspace, dev_status};
+  const hipError_t e = specdec::launch_attend(p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "attention launch");
+  return ok();
+}
+
+}  // namespace
+
+specdec_status_t specdec_append_window(const void* qkv, int32_t dtype, int32_t T, int32_t Hq, const void* q_norm,
+                                       const void* k_norm, float eps, const float* inv_freq, int32_t n_freq,
+                                       int32_t adjacent, const specdec_kv_t* kv, int32_t layer, int32_t W_in,
+                                       const int32_t* pad_in, void* q_out, uint32_t* dev_status, void* stream) {
+  specdec::CacheView c{};
+  specdec_status_t s = check_window(kv, "kv", layer, kv ? kv->B : 0, T, Hq, &c);
+  if (!s) s = check_batch(kv, T, W_in, pad_in, &c);
+  return s ? s : append(qkv, dtype, kv->B, T, Hq, q_norm, k_norm, eps, inv_freq, n_freq, adjacent, kv, c, q_out, dev_status, stream);
+}
+
+specdec_status_t specdec_append_paged(const void* qkv, int32_t dtype, int32_t B, int32_t T, int32_t Hq,
+                                      const void* q_norm, const void* k_norm, float eps, const float* inv_freq,
+                                      int32_t n_freq, int32_t adjacent, const specdec_kv_t* pool, int32_t layer,
+                                      const int32_t* table, int64_t table_stride, const int32_t* lens, void* q_out,
+                                      uint32_t* dev_status, void* stream) {
+  specdec::CacheView c{};
+  specdec_status_t s = check_window(pool, "pool", layer, B, T, Hq, &c);
+  if (!s) s = check_pages(pool, B, T, table, table_stride, lens, 0, &c);
+  return s ? s : append(qkv, dtype, B, T, Hq, q_norm, k_norm, eps, inv_freq, n_freq, adjacent, pool, c, q_out, dev_status, stream);
+}
+
+size_t specdec_attend_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t H, int32_t D, int32_t max_len) {
+  if (B < 0 || B > SPECDEC_MAX_B || T < 1 || T > SPECDEC_MAX_K + 1 || static_cast<int64_t>(B) * T > SPECDEC_MAX_ROWS ||
+      H < 1 || Hq < 1 || Hq > SPECDEC_MAX_ROWS || Hq % H != 0 || D < 8 || D > SPECDEC_MAX_HEAD_D || D % 8 != 0 ||
+      max_len < T || max_len > SPECDEC_MAX_WIDTH)
+    return 0;
+  return static_cast<size_t>(specdec::attend_workspace(B, T, Hq, H, D, max_len));
+}
+
+specdec_status_t specdec_attend_window(const void* q, int32_t T, int32_t Hq, float scale, const specdec_kv_t* kv,
+                                       int32_t layer, int32_t W_in, const int32_t* pad_in, void* out, void* workspace,
+                                       size_t workspace_bytes, uint32_t* dev_status, void* stream) {
+  specdec::CacheView c{};
+  specdec_status_t s = check_window(kv, "kv", layer, kv ? kv->B : 0, T, Hq, &c);
+  if (!s) s = check_batch(kv, T, W_in, pad_in, &c);
+  return s ? s : attend(q, kv->B, T, Hq, scale, kv, c, out, workspace, workspace_bytes, dev_status, stream);
+}
+
+specdec_status_t specdec_attend_paged(const void* q, int32_t B, int32_t T, int32_t Hq, float scale,
+                                      const specdec_kv_t* pool, int32_t layer, const int32_t* table,
+                                      int64_t table_stride, const int32_t* lens, int32_t max_len, void* out,
+                                      void* workspace, size_t workspace_bytes, uint32_t* dev_status, void* stream) {
+  specdec::CacheView c{};
+  specdec_status_t s = check_window(pool, "pool", layer, B, T, Hq, &c);
+  if (!s && max_len < T) s = fail(SPECDEC_ERR_INVALID_ARGUMENT, "max_len=%d < T=%d", max_len, T);
+  if (!s) s = check_pages(pool, B, T, table, table_stride, lens, max_len, &c);
+  return s ? s : attend(q, B, T, Hq, scale, pool, c, out, workspace, workspace_bytes, dev_status, stream);
+}
+
+specdec_status_t specdec_process_logits(const void* logits, void* out, int32_t dtype, int32_t B, int32_t k, int32_t V,
+                                        const int32_t* s, int64_t s_stride, int32_t width, const int32_t* draft,
+                                        const int32_t* begin, const int32_t* lens, const int32_t* prompt,
+                                        const float* repetition, const float* presence, const float* frequency,
+                                        const int32_t* bias_ids, const float* bias, int32_t n_bias,
+                                        const uint32_t* mask, int64_t mask_stride, uint32_t* dev_status, void* stream) {
+  if (B < 0 || B > SPECDEC_MAX_B) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "B=%d outside [0,%d]", B, SPECDEC_MAX_B);
+  if (k < 0 || k > SPECDEC_MAX_K) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "k=%d outside [0,%d]", k, SPECDEC_MAX_K);
+  if (V < 1) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "V=%d must be >= 1", V);
+  const int eb = logit_bytes(dtype);
+  if (eb == 0) return fail(SPECDEC_ERR_UNSUPPORTED, "logit dtype %d not supported", dtype);
+  const int64_t rows = static_cast<int64_t>(B) * (k + 1);
+  if (rows > SPECDEC_MAX_ROWS) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "B*(k+1)=%lld exceeds %d", (long long)rows, SPECDEC_MAX_ROWS);
+  if (n_bias < 0 || n_bias > SPECDEC_MAX_BIAS)
+    return fail(SPECDEC_ERR_INVALID_ARGUMENT, "n_bias=%d outside [0,%d]", n_bias, SPECDEC_MAX_BIAS);
+  const bool penalties = repetition || presence || frequency;
+  const int64_t words = (static_cast<int64_t>(V) + 31) / 32;
+  if (penalties && (s_stride < 1 || s_stride > SPECDEC_MAX_WIDTH + 1))
+    return fail(SPECDEC_ERR_INVALID_ARGUMENT, "s_stride=%lld outside [1,%d]", (long long)s_stride, SPECDEC_MAX_WIDTH + 1);
+  if (penalties && !lens && (width < 0 || width >= s_stride))
+    return fail(SPECDEC_ERR_INVALID_ARGUMENT, "width=%d outside [0, s_stride=%lld)", width, (long long)s_stride);
+  if (mask && (mask_stride < words || mask_stride > 0x7FFFFFFFLL))
+    return fail(SPECDEC_ERR_INVALID_ARGUMENT, "mask_stride=%lld < %lld words of V=%d", (long long)mask_stride, (long long)words, V);
+  if (B == 0) return ok();
+  if (!logits || !out) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "NULL logits / out");
+  if (penalties && (!s || (k > 0 && !draft))) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "penalties need s and draft");
+  if (n_bias > 0 && (!bias_ids || !bias)) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "NULL bias_ids / bias");
+  if (!aligned(logits, eb) || !aligned(out, eb)) return fail(SPECDEC_ERR_UNSUPPORTED, "logits / out not aligned to %d bytes", eb);
+  const void* words4[] = {s, draft, begin, lens, prompt, repetition, presence, frequency, bias_ids, bias, mask, dev_status};
+  for (const void* p : words4)
+    if (p && !aligned(p, 4)) return fail(SPECDEC_ERR_UNSUPPORTED, "4-byte tensor not 4-byte aligned");
+  {
+    const int64_t b4 = 4 * static_cast<int64_t>(B), all = rows * V * eb;
+    const specdec_status_t d = check_disjoint(
+        {{out == logits ? nullptr : logits, all, "logits"}, {penalties ? s : nullptr, b4 * s_stride, "s"},
+         {draft, b4 * k, "draft"}, {begin, b4, "begin"}, {lens, b4, "lens"}, {prompt, b4, "prompt"},
+         {repetition, b4, "repetition"}, {presence, b4, "presence"}, {frequency, b4, "frequency"},
+         {bias_ids, b4 * n_bias, "bias_ids"}, {bias, b4 * n_bias, "bias"}, {mask, 4 * rows * mask_stride, "mask"}},
+        {{out, all, "out"}, {dev_status, 4, "dev_status"}});
+    if (d) return d;
+  }
+  const specdec::LogitsLaunch p{logits, out, dtype, B, k, V, s, s_stride, width, draft, begin, lens, prompt, repetition,
+                                presence, frequency, bias_ids, bias, n_bias, mask, mask_stride, dev_status};
+  const hipError_t e = specdec::launch_logits(p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "logits launch");
+  return ok();
+}
+
 specdec_status_t specdec_timing_enable(int32_t kernel_mask) {
   if (kernel_mask < 0 || kernel_mask > SPECDEC_TIMING_ALL)
     return fail(SPECDEC_ERR_INVALID_ARGUMENT, "timing mask %d outside [0,%d]", kernel_mask, SPECDEC_TIMING_ALL);

@@ -213,6 +213,78 @@ hipError_t launch_varlen_rollback(const VarlenLaunch& p, hipStream_t stream);
 hipError_t launch_gather(const GatherLaunch& p, hipStream_t stream);
 hipError_t launch_writeback(const WritebackLaunch& p, hipStream_t stream);
 
+// One layer of a cache as the forward-side kernels see it: a left-padded
+// batch (table NULL: `lens` holds the paddings, `width` the batch's width with
+// the window) or pages of a pool (`lens` the entries before the window,
+// `width` the bound on entries with the window).
+struct CacheView {
+  void* k;                   // [rows][H][cap][D] bf16 of the layer
+  void* v;
+  int32_t rows;              // batch rows, or pages of the pool
+  int32_t H, D;
+  int64_t cap;               // columns of a row, or entries of a page
+  int64_t row_stride;        // H * cap * D elements
+  const int32_t* table;      // [B][table_stride] page ids, or NULL
+  int64_t table_stride;
+  const int32_t* lens;       // [B]
+  int32_t width;
+};
+
+// Norms, rotation and append of one window (T tokens a sequence).
+struct AppendLaunch {
+  const void* qkv;           // [B][T][Hq + 2H][D]
+  int dtype;
+  int32_t B, T, Hq;
+  const void* q_norm;        // [D] of the same type, or NULL
+  const void* k_norm;
+  float eps;
+  const float* inv_freq;     // [half], or NULL with half = 0
+  int32_t half;              // rotated pairs
+  bool adjacent;             // pairs (2j, 2j+1) rather than (j, j + half)
+  CacheView cache;
+  void* q_out;               // bf16 [B][T][Hq][D]
+  uint32_t* dev_status;
+};
+hipError_t launch_append(const AppendLaunch& p, hipStream_t stream);
+
+// Attention of one window over the cache.
+struct AttendLaunch {
+  const void* q;             // bf16 [B][T][Hq][D]
+  int32_t B, T, Hq;
+  float scale;
+  CacheView cache;
+  void* out;                 // bf16 [B][T][Hq][D]
+  void* workspace;
+  uint32_t* dev_status;
+};
+int64_t attend_workspace(int64_t B, int64_t T, int64_t Hq, int64_t H, int64_t D, int64_t max_len);
+hipError_t launch_attend(const AttendLaunch& p, hipStream_t stream);
+
+// Penalties, biases and masks on the logits of a window.
+struct LogitsLaunch {
+  const void* logits;        // [B][k+1][V]
+  void* out;                 // the same buffer: in place
+  int dtype;
+  int32_t B, k, V;
+  const int32_t* s;          // [B][s_stride] token rows
+  int64_t s_stride;
+  int32_t width;
+  const int32_t* draft;      // [B][k]
+  const int32_t* begin;      // [B] or NULL
+  const int32_t* lens;       // [B] or NULL
+  const int32_t* prompt;     // [B] or NULL
+  const float* repetition;   // [B] or NULL
+  const float* presence;
+  const float* frequency;
+  const int32_t* bias_ids;   // [B][n_bias]
+  const float* bias;
+  int32_t n_bias;
+  const uint32_t* mask;      // [B][k+1][mask_stride] or NULL
+  int64_t mask_stride;
+  uint32_t* dev_status;
+};
+hipError_t launch_logits(const LogitsLaunch& p, hipStream_t stream);
+
 // Message of the calling thread's last failure (specdec_last_error), for
 // entry points defined outside the main API source.
 void set_last_error(const char* msg);

@@ -30,7 +30,7 @@ KERNEL_VERIFY, KERNEL_REALIGN, KERNEL_POSMASK, KERNEL_GATHER, KERNEL_WRITEBACK, 
 KERNEL_VARLEN, KERNEL_VERIFY_SCAN, KERNEL_SAMPLE_STATS = 6, 7, 8
 TIMING_ALL = 511
 DEV_BAD_PAD_IN, DEV_BAD_ACCEPT, DEV_BAD_WIDTH, DEV_BAD_PAD_OUT = 1, 2, 4, 8
-DEV_BAD_SLOT, DEV_SLOT_LEN, DEV_BAD_UNIFORM = 0x10, 0x20, 0x40
+DEV_BAD_SLOT, DEV_SLOT_LEN, DEV_BAD_UNIFORM, DEV_EMPTY_MASK = 0x10, 0x20, 0x40, 0x80
 WRITEBACK_FULL, WRITEBACK_APPEND = 0, 1
 
 EXPORTED = (
@@ -38,6 +38,8 @@ EXPORTED = (
     "specdec_verify_greedy", "specdec_sample_workspace_bytes", "specdec_verify_sample", "specdec_realign_kv", "specdec_build_posmask", "specdec_realign_tokens",
     "specdec_step", "specdec_step_noalloc", "specdec_step_sample", "specdec_gather_batch", "specdec_scatter_accepted",
     "specdec_rollback", "specdec_varlen_rollback",
+    "specdec_append_window", "specdec_append_paged", "specdec_attend_workspace_bytes", "specdec_attend_window",
+    "specdec_attend_paged", "specdec_process_logits",
     "specdec_sched_create", "specdec_sched_destroy", "specdec_sched_next_batch", "specdec_sched_commit",
     "specdec_sched_lengths", "specdec_sched_active",
     "specdec_timing_enable", "specdec_timing_reset", "specdec_timing_query",
@@ -98,6 +100,15 @@ def _load(path: Path = _LIB_PATH) -> ctypes.CDLL:
     lib.specdec_varlen_rollback.argtypes = [pVL, pVL, P, P, i32, i32, i32, P, P, i64, P, P]
     lib.specdec_gather_batch.argtypes = [pKV, P, i64, P, P, i32, i32, i32, pKV, P, i64, i32, P, P, P, i64, P, P]
     lib.specdec_scatter_accepted.argtypes = [pKV, P, P, P, P, i32, i32, i32, pKV, P, i64, P, P, i64, i32, P, P]
+    f32 = ctypes.c_float
+    lib.specdec_append_window.argtypes = [P, i32, i32, i32, P, P, f32, P, i32, i32, pKV, i32, i32, P, P, P, P]
+    lib.specdec_append_paged.argtypes = [P, i32, i32, i32, i32, P, P, f32, P, i32, i32, pKV, i32, P, i64, P, P, P, P]
+    lib.specdec_attend_workspace_bytes.argtypes = [i32] * 6
+    lib.specdec_attend_workspace_bytes.restype = sz
+    lib.specdec_attend_window.argtypes = [P, i32, i32, f32, pKV, i32, i32, P, P, P, sz, P, P]
+    lib.specdec_attend_paged.argtypes = [P, i32, i32, i32, f32, pKV, i32, P, i64, P, i32, P, P, sz, P, P]
+    lib.specdec_process_logits.argtypes = [P, P, i32, i32, i32, i32, P, i64, i32, P, P, P, P, P, P, P, P, P, i32, P, i64, P,
+                                           P]
     lib.specdec_sched_create.argtypes = [P, i32, i32, i32, i32, i32, i32, ctypes.POINTER(P)]
     lib.specdec_sched_destroy.argtypes = [P]
     lib.specdec_sched_destroy.restype = None
@@ -112,7 +123,8 @@ def _load(path: Path = _LIB_PATH) -> ctypes.CDLL:
                  "specdec_build_posmask", "specdec_realign_tokens", "specdec_step", "specdec_timing_enable",
                  "specdec_timing_reset", "specdec_timing_query", "specdec_gather_batch",
                  "specdec_scatter_accepted", "specdec_sched_create", "specdec_sched_next_batch", "specdec_verify_sample",
-                 "specdec_step_sample", "specdec_rollback", "specdec_varlen_rollback",
+                 "specdec_step_sample", "specdec_rollback", "specdec_varlen_rollback", "specdec_append_window",
+                 "specdec_append_paged", "specdec_attend_window", "specdec_attend_paged", "specdec_process_logits",
                  "specdec_sched_commit", "specdec_sched_lengths"):
         getattr(lib, name).restype = ctypes.c_int
     return lib
@@ -640,6 +652,169 @@ def specdec_varlen_rollback(src, dst, cu_in, n_acc, k: int, max_len: int, cu_out
     _check(lib.specdec_varlen_rollback(ctypes.byref(s), ctypes.byref(d), _p(cu_in), _p(n_acc), B, k, max_len,
                                        _p(cu_out), _p(pos), pos.numel() if pos is not None else 0, _p(dev_status),
                                        _stream(stream)))
+
+
+def _on_current_device(name, t):
+    """The kernels run on the current device."""
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _check_append(qkv, kv, q_out, inv_freq, q_norm, k_norm, dev_status):
+    """The arguments that both appends share: (B, T, Hq, descriptor of the cache)."""
+    if qkv.dim() != 4 or qkv.dtype not in DTYPE_OF or not qkv.is_cuda or not qkv.is_contiguous():
+        raise ValueError("qkv must be a contiguous device tensor [B][T][Hq+2H][D] of float32/bfloat16/float16")
+    _on_current_device("qkv", qkv)
+    d = kv_desc(kv)
+    B, T, heads, D = qkv.shape
+    Hq = heads - 2 * d.H
+    if D != d.D or Hq < 1:
+        raise ValueError("qkv's heads do not fit the cache's")
+    _req("q_out", q_out, (B, T, Hq, D), torch.bfloat16)
+    _req("q_norm", q_norm, (D,), qkv.dtype, optional=True)
+    _req("k_norm", k_norm, (D,), qkv.dtype, optional=True)
+    _req("inv_freq", inv_freq, (inv_freq.numel() if inv_freq is not None else 0,), torch.float32, optional=True)
+    _req("dev_status", dev_status, (1,), torch.int32, optional=True)
+    return B, T, Hq, d
+
+
+def specdec_append_window(qkv, kv, layer: int, W_in: int, pad_in, q_out, inv_freq=None, q_norm=None, k_norm=None,
+                          eps: float = 1e-6, adjacent: bool = False, dev_status=None, stream=None) -> None:
+    """Norms of queries and keys, position rotation, and the window's keys and
+    values appended to columns [W_in - T, W_in) of a left-padded cache's layer;
+    ``qkv`` [B][T][Hq+2H][D] are the projections, ``q_out`` bf16 [B][T][Hq][D]."""
+    if _native is not None:
+        r = _native.append_window(qkv, kv, layer, W_in, pad_in, q_out, inv_freq, q_norm, k_norm, eps, adjacent,
+                                  dev_status, _raw(stream))
+        if r is not NotImplemented:
+            return _check(r)
+    B, T, Hq, d = _check_append(qkv, kv, q_out, inv_freq, q_norm, k_norm, dev_status)
+    if d.B != B:
+        raise ValueError("cache rows differ from qkv's")
+    _req("pad_in", pad_in, (B,), torch.int32)
+    _check(lib.specdec_append_window(_p(qkv), DTYPE_OF[qkv.dtype], T, Hq, _p(q_norm), _p(k_norm), float(eps),
+                                     _p(inv_freq), inv_freq.numel() if inv_freq is not None else 0, 1 if adjacent else 0,
+                                     ctypes.byref(d), layer, W_in, _p(pad_in), _p(q_out), _p(dev_status),
+                                     _stream(stream)))
+
+
+def specdec_append_paged(qkv, pool, layer: int, table, lens, q_out, inv_freq=None, q_norm=None, k_norm=None,
+                         eps: float = 1e-6, adjacent: bool = False, dev_status=None, stream=None) -> None:
+    """``specdec_append_window`` on pages: entry j of sequence i lies in page
+    ``table[i][j // P]`` of the pool [L][2][N][H][P][D], and the window's are
+    entries lens[i] .. lens[i] + T - 1."""
+    if _native is not None:
+        r = _native.append_paged(qkv, pool, layer, table, lens, q_out, inv_freq, q_norm, k_norm, eps, adjacent,
+                                 dev_status, _raw(stream))
+        if r is not NotImplemented:
+            return _check(r)
+    B, T, Hq, d = _check_append(qkv, pool, q_out, inv_freq, q_norm, k_norm, dev_status)
+    _req("table", table, (B, table.shape[1]), torch.int32)
+    _req("lens", lens, (B,), torch.int32)
+    _check(lib.specdec_append_paged(_p(qkv), DTYPE_OF[qkv.dtype], B, T, Hq, _p(q_norm), _p(k_norm), float(eps),
+                                    _p(inv_freq), inv_freq.numel() if inv_freq is not None else 0, 1 if adjacent else 0,
+                                    ctypes.byref(d), layer, _p(table), table.shape[1], _p(lens), _p(q_out),
+                                    _p(dev_status), _stream(stream)))
+
+
+def attend_workspace_bytes(B: int, T: int, Hq: int, H: int, D: int, max_len: int) -> int:
+    return lib.specdec_attend_workspace_bytes(B, T, Hq, H, D, max_len)
+
+
+def alloc_attend_workspace(B: int, T: int, Hq: int, H: int, D: int, max_len: int, device="cuda") -> torch.Tensor:
+    """A workspace tensor for specdec_attend_window (max_len = W_in) and
+    specdec_attend_paged (needs no initialisation)."""
+    n = attend_workspace_bytes(B, T, Hq, H, D, max_len)
+    return torch.empty((n + 15) // 16 * 2, dtype=torch.int64, device=device)
+
+
+def _check_attend(q, kv, out, workspace, max_len, dev_status):
+    """The arguments that both attentions share: (B, T, Hq, descriptor of the cache, bytes of the workspace)."""
+    if q.dim() != 4:
+        raise ValueError("q must be [B][T][Hq][D]")
+    d = kv_desc(kv)
+    B, T, Hq, D = q.shape
+    if D != d.D:
+        raise ValueError("q's head size differs from the cache's")
+    _req("q", q, (B, T, Hq, D), torch.bfloat16)
+    _on_current_device("q", q)
+    _req("out", out, (B, T, Hq, D), torch.bfloat16)
+    _req("dev_status", dev_status, (1,), torch.int32, optional=True)
+    nb = workspace.numel() * workspace.element_size()
+    if nb < attend_workspace_bytes(B, T, Hq, d.H, D, max_len) or not workspace.is_cuda:
+        raise ValueError("workspace too small")
+    return B, T, Hq, d, nb
+
+
+def specdec_attend_window(q, kv, layer: int, W_in: int, pad_in, out, workspace, scale: float | None = None,
+                          dev_status=None, stream=None) -> None:
+    """Attention of the window's queries [B][T][Hq][D] over each sequence's
+    cached entries and the window up to the query itself, on one layer of a
+    left-padded cache; ``scale`` defaults to 1 / sqrt(D)."""
+    if _native is not None:
+        r = _native.attend_window(q, kv, layer, W_in, pad_in, out, workspace, scale, dev_status, _raw(stream))
+        if r is not NotImplemented:
+            return _check(r)
+    B, T, Hq, d, nb = _check_attend(q, kv, out, workspace, W_in, dev_status)
+    if d.B != B:
+        raise ValueError("cache rows differ from q's")
+    _req("pad_in", pad_in, (B,), torch.int32)
+    _check(lib.specdec_attend_window(_p(q), T, Hq, d.D ** -0.5 if scale is None else float(scale), ctypes.byref(d), layer,
+                                     W_in, _p(pad_in), _p(out), _p(workspace), nb, _p(dev_status), _stream(stream)))
+
+
+def specdec_attend_paged(q, pool, layer: int, table, lens, max_len: int, out, workspace, scale: float | None = None,
+                         dev_status=None, stream=None) -> None:
+    """``specdec_attend_window`` on pages (see ``specdec_append_paged``);
+    ``max_len`` is a host bound on lens[i] + T."""
+    if _native is not None:
+        r = _native.attend_paged(q, pool, layer, table, lens, max_len, out, workspace, scale, dev_status, _raw(stream))
+        if r is not NotImplemented:
+            return _check(r)
+    B, T, Hq, d, nb = _check_attend(q, pool, out, workspace, max_len, dev_status)
+    _req("table", table, (B, table.shape[1]), torch.int32)
+    _req("lens", lens, (B,), torch.int32)
+    _check(lib.specdec_attend_paged(_p(q), B, T, Hq, d.D ** -0.5 if scale is None else float(scale), ctypes.byref(d),
+                                    layer, _p(table), table.shape[1], _p(lens), max_len, _p(out), _p(workspace), nb,
+                                    _p(dev_status), _stream(stream)))
+
+
+def specdec_process_logits(logits, out, s=None, width: int = 0, draft=None, begin=None, lens=None, prompt=None,
+                           repetition=None, presence=None, frequency=None, bias_ids=None, bias=None, mask=None,
+                           dev_status=None, stream=None) -> None:
+    """Penalties, biases and a grammar mask on the logits [B][k+1][V] of a
+    window, into ``out`` (or in place, ``out`` = ``logits``).  ``s`` int32
+    [B][stride] are the token rows: row i's history is columns begin[i] ..
+    lens[i] (``width`` for every row without ``lens``), then the drafts before
+    the slot.  ``mask`` int32 [B][k+1][words] holds one bit a token."""
+    if _native is not None:
+        r = _native.process_logits(logits, out, s, width, draft, begin, lens, prompt, repetition, presence, frequency,
+                                   bias_ids, bias, mask, dev_status, _raw(stream))
+        if r is not NotImplemented:
+            return _check(r)
+    if logits.dim() != 3 or logits.dtype not in DTYPE_OF or not logits.is_cuda or not logits.is_contiguous():
+        raise ValueError("logits must be a contiguous device tensor [B][k+1][V] of float32/bfloat16/float16")
+    _on_current_device("logits", logits)
+    B, kp1, V = logits.shape
+    _req("out", out, (B, kp1, V), logits.dtype)
+    _req("s", s, (B, s.shape[1] if s is not None else 0), torch.int32, optional=True)
+    _req("draft", draft, (B, kp1 - 1), torch.int32, optional=True)
+    for name, t, dt in (("begin", begin, torch.int32), ("lens", lens, torch.int32), ("prompt", prompt, torch.int32),
+                        ("repetition", repetition, torch.float32), ("presence", presence, torch.float32),
+                        ("frequency", frequency, torch.float32)):
+        _req(name, t, (B,), dt, optional=True)
+    if (bias_ids is None) != (bias is None):
+        raise ValueError("give both bias_ids and bias, or neither")
+    n_bias = bias_ids.shape[1] if bias_ids is not None else 0
+    _req("bias_ids", bias_ids, (B, n_bias), torch.int32, optional=True)
+    _req("bias", bias, (B, n_bias), torch.float32, optional=True)
+    words = mask.shape[2] if mask is not None else 0
+    _req("mask", mask, (B, kp1, words), torch.int32, optional=True)
+    _req("dev_status", dev_status, (1,), torch.int32, optional=True)
+    _check(lib.specdec_process_logits(_p(logits), _p(out), DTYPE_OF[logits.dtype], B, kp1 - 1, V, _p(s),
+                                      s.shape[1] if s is not None else 0, width, _p(draft), _p(begin), _p(lens),
+                                      _p(prompt), _p(repetition), _p(presence), _p(frequency), _p(bias_ids), _p(bias),
+                                      n_bias, _p(mask), words, _p(dev_status), _stream(stream)))
 
 
 def timing_enable(on=True) -> None:

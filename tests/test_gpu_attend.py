@@ -1,0 +1,287 @@
+"""specdec_attend_window / specdec_attend_paged against a 64-bit
+implementation: head layouts and sizes, lengths from none to long, page sizes,
+values that must not be read, sequences left untouched, large scores, graph
+replays and offsets past 32 bits."""
+import numpy as np
+import pytest
+import torch
+
+from tests import forward_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def sd():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2510_22876_amd import specdec
+    yield specdec
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+
+
+def _queries(c, Hq, seed, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (scale * torch.randn((len(c.n), c.T, Hq, c.D), generator=g)).to(torch.bfloat16)
+
+
+def _run(sd, c, q, scale=None, **over):
+    out = torch.full(q.shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+    kv, status = c.kv.cuda(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    B, T, Hq, D = q.shape
+    ws = sd.alloc_attend_workspace(B, T, Hq, c.H, D, over.get("max_len", c.max_len) if c.page else c.W_in)
+    ws.fill_(-1)                                          # NaN patterns: it needs no initialisation
+    if c.page:
+        sd.specdec_attend_paged(q.cuda(), kv, c.layer, over.get("table", c.table), over.get("lens", c.lens),
+                                over.get("max_len", c.max_len), out, ws, scale, status)
+    else:
+        sd.specdec_attend_window(q.cuda(), kv, c.layer, c.W_in, over.get("pad", c.pad), out, ws, scale, status)
+    torch.cuda.synchronize()
+    return out.cpu(), int(status.cpu()[0])
+
+
+def _check(c, q, out, scale=None, skip=()):
+    scale = c.D ** -0.5 if scale is None else scale
+    for i, n in enumerate(c.n):
+        if i in skip:
+            assert bool(torch.isnan(out[i]).all()), f"row {i} was to be left untouched"
+            continue
+        k, v = c.entries(i, n + c.T)
+        want, bound = ref.attend(q[i], k, v, n, scale)
+        ref.check(out[i], want, bound, f"row {i} of {n} entries")
+
+
+CASES = {   # (Hq, H, D, T, entries, page, further columns of width)
+    "first_token": (2, 1, 64, 1, [0], 0, 0),
+    "tiny": (4, 2, 16, 5, [8, 40], 0, 17),
+    "mha": (6, 6, 128, 6, [0, 1, 31, 32, 33, 63, 64, 65, 200], 0, 0),
+    "gqa": (8, 2, 128, 8, [5, 500, 1027], 0, 0),
+    "gqa7": (14, 2, 128, 5, [100, 0, 257], 0, 3),
+    "mqa_wide": (48, 1, 64, 3, [17, 90], 0, 0),
+    "one_paged": (32, 8, 128, 1, [1000], 16, 0),
+    "one_token_ragged": (4, 4, 128, 1, [0, 1, 15, 16, 17, 127, 128, 129, 2500], 0, 0),
+    "page1": (2, 2, 32, 2, [0, 3, 40], 1, 0),
+    "page3": (4, 2, 64, 4, [1, 2, 70], 3, 0),
+    "page16": (4, 1, 128, 6, [15, 16, 300], 16, 0),
+    "page24": (4, 2, 128, 3, [23, 24, 25, 400], 24, 0),
+    "page48": (4, 2, 128, 3, [47, 48, 700], 48, 0),
+    "page64": (8, 2, 128, 8, [56, 57, 63, 64, 900], 64, 0),
+    "page100": (2, 1, 128, 2, [99, 350], 100, 0),
+    "pool_slots": (4, 2, 128, 4, [50, 20, 64], 68, 0),
+    "d8": (2, 1, 8, 3, [4, 50], 0, 0),
+    "d24": (3, 3, 24, 2, [30, 77], 5, 0),
+    "d72": (2, 2, 72, 2, [30, 131], 0, 0),
+    "d80": (12, 12, 80, 4, [10, 333], 32, 0),
+    "d96": (16, 2, 96, 1, [64, 640], 0, 0),
+    "d136": (2, 1, 136, 2, [33, 260], 16, 0),
+    "d256": (8, 2, 256, 3, [100, 600], 0, 0),
+    "long_window": (8, 2, 128, 65, [0, 100], 0, 0),
+    "long_window_gqa7": (14, 2, 64, 65, [3, 200], 16, 0),
+    "wide_window_one_head": (1, 1, 128, 33, [70], 64, 0),
+    "long": (4, 2, 128, 2, [12345], 0, 0),
+    "long_paged": (8, 1, 64, 3, [20011, 5], 128, 0),
+    "long_d256": (2, 1, 256, 1, [9000], 16, 0),
+}
+
+
+@pytest.mark.parametrize("name", CASES)
+def test_matches_64_bits(sd, name):
+    Hq, H, D, T, n, page, more = CASES[name]
+    c = ref.Cache(n, T, H, D, page, slots=name == "pool_slots", width=max(n) + T + more)
+    c.fill(T, torch.Generator().manual_seed(1))
+    q = _queries(c, Hq, 2, 2.0)
+    out, status = _run(sd, c, q)
+    assert status == 0
+    _check(c, q, out)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1.0, 40.0])
+def test_scales_and_large_scores(sd, scale):
+    """No weighting at all, inverted, and scores of several thousand, where all the weight falls on one entry."""
+    c = ref.Cache([700, 3], 3, 2, 128)
+    c.fill(3, torch.Generator().manual_seed(1))
+    q = _queries(c, 4, 3, 3.0)
+    out, _ = _run(sd, c, q, scale)
+    _check(c, q, out, scale)
+
+
+def test_max_len_beyond_the_lengths(sd):
+    """A loose bound on the lengths changes how the work is split, not what is read or answered."""
+    c = ref.Cache([10, 0, 130], 2, 2, 64, 16)
+    c.table_np = np.pad(c.table_np, ((0, 0), (0, 3000)), constant_values=-1)
+    c.table = torch.as_tensor(c.table_np, device="cuda")
+    c.fill(2, torch.Generator().manual_seed(1))
+    q = _queries(c, 4, 3)
+    for max_len in (132, 1000, 48000):
+        out, status = _run(sd, c, q, max_len=max_len)
+        assert status == 0
+        _check(c, q, out)
+
+
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("bad", ["nan_value", "inf_value", "nan_key", "inf_key"])
+def test_later_window_entries_are_not_read(sd, page, bad):
+    """NaN and infinities in the window's later entries reach no earlier query."""
+    n, T = [40, 0, 61], 5
+    c = ref.Cache(n, T, 2, 64, page)
+    c.fill(T, torch.Generator().manual_seed(1))
+    for i, x in enumerate(n):
+        row, col = c.where(i, x + 3)
+        c.kv[c.layer, 1 if "value" in bad else 0, row, 1, col, 5] = float(bad[:3])
+    q = _queries(c, 4, 3)
+    out, _ = _run(sd, c, q)
+    assert bool(torch.isfinite(out[:, :3]).all()) and bool(torch.isfinite(out[:, :, :2]).all())
+    for i, x in enumerate(n):
+        k, v = c.entries(i, x + T)
+        want, bound = ref.attend(q[i], k, v, x, 0.125)
+        ref.check(out[i][:3], want[:3], bound[:3], "before")
+        ref.check(out[i][:, :2], want[:, :2], bound[:, :2], "the other head")
+        if "value" in bad:                                # element 5 of head 1's queries from slot 3 on, and no other
+            late, lb = want[3:, 2:].clone(), bound[3:, 2:]
+            got = out[i][3:, 2:].double()
+            assert not bool(torch.isfinite(got[..., 5]).any())
+            late[..., 5] = got[..., 5] = 0
+            ref.check(got, late, torch.nan_to_num(lb), "the other elements")
+
+
+@pytest.mark.parametrize("page", [0, 8])
+def test_infinite_keys_among_the_cached(sd, page):
+    """A score of -inf has no weight, wherever it stands; a sequence of nothing else has none to give."""
+    c = ref.Cache([90, 2], 1, 1, 32, page)
+    c.fill(1, torch.Generator().manual_seed(1))
+    q = _queries(c, 1, 3)
+    q[..., 0] = -1.0
+    for j in list(range(0, 64)) + [80]:
+        row, col = c.where(0, j)
+        c.kv[c.layer, 0, row, 0, col, 0] = float("inf")
+    for j in range(3):
+        row, col = c.where(1, j)
+        c.kv[c.layer, 0, row, 0, col, 0] = float("inf")
+    out, _ = _run(sd, c, q)
+    k, v = c.entries(0, 91)
+    keep = torch.isfinite(k[:, 0, 0])
+    want, bound = ref.attend(q[0], k[keep], v[keep], int(keep.sum()) - 1, 32 ** -0.5)
+    ref.check(out[0], want, bound, "row 0")
+    assert bool(torch.isnan(out[1]).all())
+
+
+@pytest.mark.parametrize("page", [0, 4, 16])
+def test_sequences_out_of_range_are_left_alone(sd, page):
+    n, T = [50, 30, 0, 60, 20], 3
+    c = ref.Cache(n, T, 2, 32, page, room=2)
+    c.fill(T, torch.Generator().manual_seed(1))
+    q = _queries(c, 4, 5)
+    if page:
+        table, lens = c.table_np.copy(), np.asarray(n, np.int32)
+        lens[0] = -1
+        lens[1] = c.max_len - T + 1
+        table[3, 62 // page] = c.shape[2]                 # the page of the last entry
+        table[4, 0] = -1
+        out, status = _run(sd, c, q, table=torch.as_tensor(table, device="cuda"), lens=torch.as_tensor(lens, device="cuda"))
+        assert status == sd.DEV_BAD_SLOT
+        _check(c, q, out, skip=(0, 1, 3, 4))
+    else:
+        pad = c.pad_np.copy()
+        pad[0], pad[3] = -1, c.W_in - T + 1
+        out, status = _run(sd, c, q, pad=torch.as_tensor(pad, device="cuda"))
+        assert status == sd.DEV_BAD_PAD_IN
+        _check(c, q, out, skip=(0, 3))
+
+
+def test_a_bad_page_far_into_a_long_sequence(sd):
+    """Every workgroup of the sequence has to leave it alone, also those that read good pages only."""
+    c = ref.Cache([9000, 100], 2, 1, 64, 16)
+    c.fill(2, torch.Generator().manual_seed(1))
+    q = _queries(c, 2, 5)
+    table = c.table_np.copy()
+    table[0, 400] = -3
+    out, status = _run(sd, c, q, table=torch.as_tensor(table, device="cuda"))
+    assert status == sd.DEV_BAD_SLOT
+    _check(c, q, out, skip=(0,))
+
+
+def test_split_over_launches(sd, monkeypatch):
+    for n, page in (([100, 3, 50, 700], 16), ([9000, 20, 400], 0)):
+        c = ref.Cache(n, 3, 2, 64, page)
+        c.fill(3, torch.Generator().manual_seed(1))
+        q = _queries(c, 4, 5)
+        monkeypatch.delenv("SPECDEC_MAX_LAUNCH_ITEMS", raising=False)
+        whole, _ = _run(sd, c, q)
+        monkeypatch.setenv("SPECDEC_MAX_LAUNCH_ITEMS", str(256 * 5))
+        parts, _ = _run(sd, c, q)
+        assert torch.equal(whole.view(torch.int16), parts.view(torch.int16))
+        _check(c, q, whole)
+
+
+def test_replays_of_a_captured_call(sd):
+    """Two captured calls that share a workspace, replayed in turn on new lengths and queries, with eager work between
+    the replays: every replay gives the bits of an eager call."""
+    n, T, Hq, H, D = [3000, 10, 700], 4, 8, 2, 64
+    c = ref.Cache(n, T, H, D, 16)
+    c.fill(T, torch.Generator().manual_seed(1))
+    kv = c.kv.cuda()
+    ws = sd.alloc_attend_workspace(len(n), T, Hq, H, D, c.max_len)
+    q = [_queries(c, Hq, s).cuda() for s in (1, 2)]
+    out = [torch.empty_like(t) for t in q]
+    lens = c.lens.clone()
+    graphs = []
+    for a, o in zip(q, out):
+        sd.specdec_attend_paged(a, kv, 1, c.table, lens, c.max_len, o, ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            sd.specdec_attend_paged(a, kv, 1, c.table, lens, c.max_len, o, ws)
+        graphs.append(g)
+    for step in range(4):
+        lens.copy_(torch.tensor([3000 - 977 * step, 10 - 3 * step, 700 - 100 * step], dtype=torch.int32))
+        for t, s in zip(q, (10 + step, 20 + step)):
+            t.copy_(_queries(c, Hq, s))
+        for o in out:
+            o.fill_(float("nan"))
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for a, o in zip(q, out):
+            eager = torch.empty_like(o)
+            sd.specdec_attend_paged(a, kv, 1, c.table, lens, c.max_len, eager, torch.empty_like(ws))
+            torch.cuda.synchronize()
+            assert torch.equal(o.view(torch.int16), eager.view(torch.int16)), f"replay {step}"
+
+
+def test_on_another_stream(sd):
+    c = ref.Cache([5000, 7], 2, 2, 128)
+    c.fill(2, torch.Generator().manual_seed(1))
+    q = _queries(c, 4, 5)
+    want, _ = _run(sd, c, q)
+    kv, qd = c.kv.cuda(), q.cuda()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.empty_like(qd) for _ in streams]
+    spaces = [sd.alloc_attend_workspace(2, 2, 4, 2, 128, c.W_in) for _ in streams]
+    torch.cuda.synchronize()
+    for st, o, ws in zip(streams, outs, spaces):
+        sd.specdec_attend_window(qd, kv, 1, c.W_in, c.pad, o, ws, stream=st)
+    torch.cuda.synchronize()
+    for o in outs:
+        assert torch.equal(o.cpu().view(torch.int16), want.view(torch.int16))
+
+
+def test_offsets_past_32_bits(sd):
+    """A row that starts 2^32 elements into a slab, whose entries lie 2^31 bytes further."""
+    cap, D, T, n = 1 << 23, 256, 2, 300
+    kv = torch.empty((1, 2, 3, 1, cap, D), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator().manual_seed(1)
+    e = torch.randn((2, n + T, D), generator=g).to(torch.bfloat16)
+    first = cap - n - T
+    for part in range(2):
+        kv[0, part, 2, 0, first:] = e[part].cuda()
+        kv[0, part, :2, 0, first:] = 0
+    q = torch.randn((3, T, 2, D), generator=g).to(torch.bfloat16)
+    pad = torch.full((3,), first, dtype=torch.int32, device="cuda")
+    out = torch.empty_like(q, device="cuda")
+    ws = sd.alloc_attend_workspace(3, T, 2, 1, D, cap)
+    sd.specdec_attend_window(q.cuda(), kv, 0, cap, pad, out, ws)
+    torch.cuda.synchronize()
+    want, bound = ref.attend(q[2], e[0].double()[:, None], e[1].double()[:, None], n, D ** -0.5)
+    ref.check(out[2], want, bound, "the far row")
+    assert bool((out[:2] == 0).all())
