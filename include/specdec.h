@@ -587,7 +587,7 @@ specdec_status_t specdec_varlen_rollback(const specdec_varlen_t* src, const spec
  *            pool->cap = P entries, any P >= 1): entry j of sequence i lies in
  *            page table[i][j / P] at column j % P; c_i = lens[i] entries are
  *            cached, the window's are entries lens[i] .. lens[i] + T - 1.
- *            EXSpec's pool of whole sequences is the case of one page each
+ *            N * H * P < 2^32.  EXSpec's pool of whole sequences is the case of one page each
  *            (table = slots, a stride of 1), so that a forward needs no
  *            gather.  After verification lens[i] grows by n_acc[i] + 1:
  *            rejected entries are overwritten by the next window.

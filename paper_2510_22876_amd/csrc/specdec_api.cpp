@@ -1215,6 +1215,9 @@ specdec_status_t check_pages(const specdec_kv_t* pool, int32_t B, int32_t T, con
   if (max_len < T || max_len > held || max_len > SPECDEC_MAX_WIDTH)
     return fail(SPECDEC_ERR_INVALID_ARGUMENT, "bound on entries %d outside [T=%d, table_stride*P=%lld]", max_len, T,
                 (long long)held);
+  if (static_cast<int64_t>(pool->B) * pool->H * pool->cap > 0xFFFFFFFFLL)
+    return fail(SPECDEC_ERR_UNSUPPORTED, "pool of %d pages, %d heads and %lld entries a page: more than 2^32 - 1 of a layer's keys",
+                pool->B, pool->H, (long long)pool->cap);
   if (!table || !lens) return fail(SPECDEC_ERR_INVALID_ARGUMENT, "NULL table / lens");
   if (!aligned(table, 4) || !aligned(lens, 4)) return fail(SPECDEC_ERR_UNSUPPORTED, "int32 tensor not 4-byte aligned");
   return SPECDEC_OK;
