@@ -9,123 +9,398 @@
 //   x = x + bias(v)
 //   x = allowed(v) ? x : -inf
 //
-// A workgroup takes one sequence and one chunk of the vocabulary and walks the
-// window's slots: the counts of its chunk, built once from the token row in
-// LDS, serve every slot, and each slot's draft is counted before the next.
+// Reading and writing the logits bounds it; few of them change but for the
+// mask.  A workgroup takes one sequence, one chunk of the vocabulary and some
+// of the window's slots.  It counts its chunk's tokens once, in LDS, and turns
+// the counts and biases of a lane's logits into what is taken off and added,
+// in registers, for all the slots; a lane then takes 8 logits at a time as
+// they lie in memory and copies or masks as bits those that no count or bias
+// touches.  A drafted token's count grows from slot to slot: such logits are
+// computed again from the counts.
 #include "forward_common.h"
+#include "span_copy.h"
+#include "specdec.h"
 
 namespace specdec {
 namespace {
 
 constexpr uint32_t kBadPadIn = 0x1u, kEmptyMask = 0x80u;
 constexpr uint32_t kPrompt = 0x80000000u;   // the token occurs in the prompt; the low bits count the answered ones
-constexpr int kChunk = 4096;
+constexpr int kChunk = 4096, kUnits = kChunk / 8 / kThreads;   // 8 logits a lane, kUnits times
 
 struct LogitsArgs {
   LogitsLaunch p;
   int64_t base;      // first workgroup of this launch
+  int64_t checks;    // workgroups ahead of the others that look for masks that allow nothing
   int64_t chunks;    // of the vocabulary
+  int32_t shares;    // workgroups that a window's slots are shared out to
+  int32_t slots;     // ... each
 };
 
-template <int kDtype>
+// Whether mask row `row` allows a token of the vocabulary; one wave.
+__device__ __forceinline__ void check_mask(const LogitsLaunch& p, int64_t row) {
+  const uint32_t* mask = p.mask + row * p.mask_stride;
+  const int64_t words = (static_cast<int64_t>(p.V) + 31) / 32;
+  const int lane = threadIdx.x & 63;
+  const uint32_t end = p.V % 32 ? (1u << p.V % 32) - 1u : ~0u;   // of the last word
+  for (int64_t w = lane; w - lane < words; w += 64 * 16) {
+    uint32_t any = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int64_t at = w + e * 64;
+      const uint32_t bits = mask[at < words ? at : words - 1];
+      any |= at < words - 1 ? bits : bits & end;
+    }
+    if (__any(any != 0)) return;
+  }
+  if (lane == 0 && p.dev_status) atomicOr(p.dev_status, kEmptyMask);
+}
+
+// 8 logits as they lie in memory, as words.  Units are passed by value and
+// their words selected, not indexed, so that they stay in registers.
+typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
+typedef uint32_t Words8 __attribute__((ext_vector_type(8)));
+template <typename T> struct UnitOf { typedef Words4 type; };
+template <> struct UnitOf<float> { typedef Words8 type; };
+template <typename T> using Unit = typename UnitOf<T>::type;
+
+// The first `count` of them lie within the vocabulary.
+template <typename T>
+__device__ __forceinline__ Unit<T> load_unit(const T* p, int count) {
+  Unit<T> u = {};
+  if (count >= 8) {
+    __builtin_memcpy(&u, p, sizeof(u));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 7; ++e) {
+      if (e >= count) break;
+      if constexpr (sizeof(T) == 4) u[e] = __float_as_uint(p[e]);
+      else u[e >> 1] |= static_cast<uint32_t>(__builtin_bit_cast(uint16_t, p[e])) << (e & 1) * 16;
+    }
+  }
+  return u;
+}
+template <typename T>
+__device__ __forceinline__ void store_unit(T* p, Unit<T> u, int count) {
+  if (count >= 8) {
+    __builtin_memcpy(p, &u, sizeof(u));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 7; ++e) {
+      if (e >= count) break;
+      if constexpr (sizeof(T) == 4) p[e] = __uint_as_float(u[e]);
+      else p[e] = __builtin_bit_cast(T, static_cast<uint16_t>(u[e >> 1] >> (e & 1) * 16));
+    }
+  }
+}
+
+// Logit e of a unit, and its replacement.
+template <typename T>
+__device__ __forceinline__ float take(Unit<T> u, int e) {
+  constexpr int kWords = sizeof(T) * 2;
+  const int at = sizeof(T) == 4 ? e : e >> 1;
+  uint32_t w = u[0];
+#pragma unroll
+  for (int y = 1; y < kWords; ++y) w = at == y ? u[y] : w;
+  if constexpr (sizeof(T) == 4) return __uint_as_float(w);
+  else return static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(e & 1 ? w >> 16 : w)));
+}
+template <typename T>
+__device__ __forceinline__ Unit<T> give(Unit<T> u, int e, float z) {
+  constexpr int kWords = sizeof(T) * 2;
+  const int at = sizeof(T) == 4 ? e : e >> 1;
+  uint32_t w, keep = 0;
+  if constexpr (sizeof(T) == 4) {
+    w = __float_as_uint(z);
+  } else {
+    w = __builtin_bit_cast(uint16_t, static_cast<T>(z));
+    keep = e & 1 ? 0xFFFFu : 0xFFFF0000u;
+    w = e & 1 ? w << 16 : w;
+  }
+#pragma unroll
+  for (int y = 0; y < kWords; ++y) u[y] = at == y ? (u[y] & keep) | w : u[y];
+  return u;
+}
+// All of a unit's logits, and those of them whose bit is set replaced.
+template <typename T>
+__device__ __forceinline__ void widen(Unit<T> u, float (&z)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) z[e] = take<T>(u, e);
+}
+template <typename T>
+__device__ __forceinline__ Unit<T> replaced(Unit<T> u, const float (&z)[8], uint32_t bits) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t keep = ~static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(bits), e, 1));
+    if constexpr (sizeof(T) == 4) {
+      u[e] = (u[e] & keep) | (__float_as_uint(z[e]) & ~keep);
+    } else {
+      const uint32_t half = e & 1 ? 0xFFFF0000u : 0xFFFFu, w = static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<T>(z[e]))) << (e & 1) * 16;
+      u[e >> 1] = (u[e >> 1] & (keep | ~half)) | (w & ~keep);
+    }
+  }
+  return u;
+}
+// -inf where bit e of `allowed` is clear.
+template <typename T>
+__device__ __forceinline__ Unit<T> masked(Unit<T> u, uint32_t allowed) {
+  constexpr int kWords = sizeof(T) * 2;
+#pragma unroll
+  for (int y = 0; y < kWords; ++y) {
+    uint32_t keep, inf;
+    if constexpr (sizeof(T) == 4) {
+      keep = static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(allowed), y, 1));
+      inf = 0xFF800000u;
+    } else {
+      const uint32_t low = static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(allowed), 2 * y, 1));
+      const uint32_t high = static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(allowed), 2 * y + 1, 1));
+      keep = (low & 0xFFFFu) | (high & 0xFFFF0000u);
+      inf = __builtin_bit_cast(uint16_t, static_cast<T>(-__builtin_inff())) * 0x10001u;
+    }
+    u[y] = (u[y] & keep) | (inf & ~keep);
+  }
+  return u;
+}
+
+template <int kDtype, bool kSparse>   // kSparse: there are penalties or biases
 __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
   typedef typename Element<kDtype>::type T;
-  __shared__ uint32_t s_n[kChunk];
-  __shared__ float s_bias[kChunk];
+  constexpr int kBitWords = kSparse ? kChunk / 32 : 1;
+  __shared__ __align__(16) uint32_t s_n[kSparse ? kChunk : 4];
+  __shared__ float s_bias[kSparse ? kChunk : 1];
+  __shared__ uint32_t s_touched[kBitWords], s_drafted[kBitWords], s_biased[kBitWords];
+  __shared__ int s_again;
   const LogitsLaunch& p = a.p;
-  const int64_t block = a.base + blockIdx.x, chunk = block % a.chunks, v0 = chunk * kChunk;
-  const int i = static_cast<int>(block / a.chunks), tid = threadIdx.x;
+  const int tid = threadIdx.x;
+  int64_t block = a.base + blockIdx.x;
+  if (block < a.checks) {
+    const int64_t row = block * (kThreads / 64) + wave_index();
+    if (row < static_cast<int64_t>(p.B) * (p.k + 1)) check_mask(p, row);
+    return;
+  }
+  block -= a.checks;
+  const int64_t chunk = block % a.chunks, v0 = chunk * kChunk, rest = block / a.chunks;
+  const int i = static_cast<int>(rest / a.shares), r0 = static_cast<int>(rest % a.shares) * a.slots;
+  const int r1 = r0 + a.slots < p.k + 1 ? r0 + a.slots : p.k + 1;
   const int size = static_cast<int>(p.V - v0 < kChunk ? p.V - v0 : kChunk);
   const bool penal = p.repetition || p.presence || p.frequency;
   int64_t begin = 0, end = p.width, answered = 0;   // columns of the history; the first behind the prompt
-  if (penal) {
-    if (p.begin) begin = p.begin[i];
-    if (p.lens) end = p.lens[i];
+  const int32_t* draft = p.draft + static_cast<int64_t>(i) * p.k;
+  if (kSparse && penal) {
+    if (p.begin) begin = load_invariant(p.begin + i);
+    if (p.lens) end = load_invariant(p.lens + i);
     if (begin < 0 || begin > end || end >= p.s_stride) {
-      if (chunk == 0 && tid == 0 && p.dev_status) atomicOr(p.dev_status, kBadPadIn);
+      if (chunk == 0 && r0 == 0 && tid == 0 && p.dev_status) atomicOr(p.dev_status, kBadPadIn);
       return;
     }
+    answered = begin + (p.prompt ? load_invariant(p.prompt + i) : 0);
   }
-  for (int j = tid; j < size; j += kThreads) {
-    s_n[j] = 0;
-    s_bias[j] = 0.f;
-  }
-  __syncthreads();
-  if (penal) {
-    const int32_t* s = p.s + i * p.s_stride;
-    answered = begin + (p.prompt ? p.prompt[i] : 0);
-    for (int64_t j = begin + tid; j <= end; j += kThreads) {
-      const int64_t v = s[j] - v0;
-      if (v < 0 || v >= size) continue;
-      if (j < answered) atomicOr(&s_n[v], kPrompt);
-      else atomicAdd(&s_n[v], 1u);
-    }
-  }
-  const int32_t* ids = p.bias_ids + static_cast<int64_t>(i) * p.n_bias;
-  const float* bias = p.bias + static_cast<int64_t>(i) * p.n_bias;
-  for (int j = tid; j < p.n_bias; j += kThreads) {
-    const int64_t v = ids[j] - v0;
-    if (v < 0 || v >= size) continue;
-    // an id given more than once: its first place adds them up, in their order
-    bool first = true;
-    for (int e = 0; e < j; ++e) first = first && ids[e] != ids[j];
-    if (!first) continue;
-    float sum = bias[j];
-    for (int e = j + 1; e < p.n_bias; ++e)
-      if (ids[e] == ids[j]) sum += bias[e];
-    s_bias[v] = sum;
-  }
-  const float rep = p.repetition ? p.repetition[i] : 1.f, pres = p.presence ? p.presence[i] : 0.f;
-  const float freq = p.frequency ? p.frequency[i] : 0.f;
   const bool in_place = p.out == p.logits;
-  for (int r = 0; r <= p.k; ++r) {
+
+  // A lane's logits are read one slot ahead, and their mask two, which says
+  // whether they are needed.
+  static_assert(kUnits == 2, "the units are written out");
+  const int64_t row0 = static_cast<int64_t>(i) * (p.k + 1);
+  const int at[2] = {tid * 8, (tid + kThreads) * 8};   // first logit of a lane's units, from v0 on
+  uint32_t touched[2] = {};                            // those that a count, a draft or a bias may change
+  auto read_mask = [&](int r, int e) -> uint32_t {
+    if (!p.mask || at[e] >= size) return 0xFFu;
+    const uint8_t* bits = reinterpret_cast<const uint8_t*>(p.mask + (row0 + (r < r1 ? r : r1 - 1)) * p.mask_stride) + v0 / 8;
+    return bits[at[e] >> 3];
+  };
+  auto needed = [&](int e, uint32_t mask) { return at[e] < size && !(in_place && mask == 0xFFu && touched[e] == 0); };
+  auto read = [&](int r, int e, uint32_t mask, Unit<T>& x) {
+    if (mask != 0 && needed(e, mask)) x = load_unit(static_cast<const T*>(p.logits) + ((row0 + r) * p.V + v0) + at[e], size - at[e]);
+  };
+  uint32_t mask0 = read_mask(r0, 0), mask1 = read_mask(r0, 1);
+  uint32_t mask0n = read_mask(r0 + 1, 0), mask1n = read_mask(r0 + 1, 1);
+  Unit<T> x0 = {}, x1 = {};
+  if (!in_place) {   // in place, the counts say which are needed
+    read(r0, 0, mask0, x0);
+    read(r0, 1, mask1, x1);
+  }
+
+  if constexpr (kSparse) {
+    const int32_t* ids = p.bias_ids + static_cast<int64_t>(i) * p.n_bias;
+    const float* bias = p.bias + static_cast<int64_t>(i) * p.n_bias;
+    uint32_t* s_place = reinterpret_cast<uint32_t*>(s_bias);
+    auto inside = [&](int32_t token) { return token >= v0 && token < v0 + size; };
+    auto mark = [](uint32_t* bits, int v) { atomicOr(&bits[v >> 5], 1u << (v & 31)); };
+    for (int j = tid; j < kChunk / 4; j += kThreads) reinterpret_cast<uint4*>(s_n)[j] = uint4{0, 0, 0, 0};
+    for (int j = tid; j < kChunk / 32; j += kThreads) s_touched[j] = s_drafted[j] = s_biased[j] = 0;
+    for (int j = tid; j < p.n_bias; j += kThreads)
+      if (inside(ids[j])) s_place[ids[j] - v0] = ~0u;
+    if (tid == 0) s_again = 0;
     __syncthreads();
-    const int64_t row = static_cast<int64_t>(i) * (p.k + 1) + r;
-    const T* x = static_cast<const T*>(p.logits) + row * p.V + v0;
-    T* y = static_cast<T*>(p.out) + row * p.V + v0;
-    const uint32_t* mask = p.mask ? p.mask + row * p.mask_stride : nullptr;
-    for (int j = tid; j < size; j += kThreads) {
-      const int64_t v = v0 + j;
-      if (mask && !(mask[v >> 5] >> (v & 31) & 1u)) {
-        y[j] = static_cast<T>(-__builtin_inff());
-        continue;
+    if (penal) {
+      const int32_t* s = p.s + i * p.s_stride;
+      auto count = [&](int64_t j, int32_t token) {
+        if (!inside(token)) return;
+        const int v = static_cast<int>(token - v0);
+        if (j < answered) atomicOr(&s_n[v], kPrompt);
+        else atomicAdd(&s_n[v], 1u);
+        mark(s_touched, v);
+      };
+      constexpr int kAhead = 8;
+      int64_t j0 = begin;
+      for (; j0 + kAhead * 4 * kThreads <= end + 1; j0 += kAhead * 4 * kThreads) {   // four tokens a load
+        int32_t token[kAhead][4];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) __builtin_memcpy(token[e], s + j0 + (e * kThreads + tid) * 4, 16);
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) count(j0 + (e * kThreads + tid) * 4 + y, token[e][y]);
       }
-      const uint32_t n = s_n[j];
-      if (in_place && n == 0 && s_bias[j] == 0.f) continue;
-      float z = static_cast<float>(x[j]);
-      if (p.repetition && n) z = z > 0.f ? z / rep : z * rep;
-      const uint32_t told = n & ~kPrompt;
-      if (told) z -= freq * static_cast<float>(told) + pres;
-      y[j] = static_cast<T>(z + s_bias[j]);
-    }
-    if (mask && chunk == 0) {   // a slot that allows nothing
-      int any = 0;
-      for (int64_t w = tid; w * 32 < p.V; w += kThreads) {
-        const uint32_t bits = p.V - w * 32 >= 32 ? ~0u : (1u << (p.V - w * 32)) - 1u;
-        any |= (mask[w] & bits) != 0;
+      for (; j0 <= end; j0 += kAhead * kThreads) {
+        int32_t token[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+          const int64_t j = j0 + e * kThreads + tid;
+          token[e] = s[j <= end ? j : end];
+        }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e)
+          if (j0 + e * kThreads + tid <= end) count(j0 + e * kThreads + tid, token[e]);
       }
-      if (!__syncthreads_or(any) && tid == 0 && p.dev_status) atomicOr(p.dev_status, kEmptyMask);
+      if (tid < r1 - 1 && inside(draft[tid])) {   // (k is below the threads)
+        mark(s_touched, static_cast<int>(draft[tid] - v0));
+        mark(s_drafted, static_cast<int>(draft[tid] - v0));
+      }
     }
+    // The biases: of an id given more than once, the first place adds all of
+    // them up, in their order.
+    constexpr int kBiases = SPECDEC_MAX_BIAS / kThreads;
+    for (int j = tid; j < p.n_bias; j += kThreads)
+      if (inside(ids[j])) atomicMin(&s_place[ids[j] - v0], static_cast<uint32_t>(j));
     __syncthreads();
-    if (penal && r < p.k && tid == 0) {
-      const int64_t v = p.draft[static_cast<int64_t>(i) * p.k + r] - v0;
-      if (v >= 0 && v < size) {
-        if (end + 1 + r < answered) s_n[v] |= kPrompt;
-        else s_n[v] += 1u;
+    if (p.n_bias > 0) {
+      bool mine[kBiases];
+#pragma unroll
+      for (int e = 0; e < kBiases; ++e) {
+        const int j = tid + e * kThreads;
+        const bool in = j < p.n_bias && inside(ids[j]);
+        mine[e] = in && s_place[ids[j] - v0] == static_cast<uint32_t>(j);
+        if (in && !mine[e]) s_again = 1;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < kBiases; ++e) {
+        if (!mine[e]) continue;
+        const int j = tid + e * kThreads, v = static_cast<int>(ids[j] - v0);
+        float sum = bias[j];
+        if (s_again)
+          for (int y = j + 1; y < p.n_bias; ++y)
+            if (ids[y] == ids[j]) sum += bias[y];
+        s_bias[v] = sum;
+        mark(s_touched, v);
+        mark(s_biased, v);
+      }
+      __syncthreads();
+    }
+  }
+  // What the counts and biases do to a lane's logits: `held` bits say where the
+  // repetition penalty applies, `add` is added.
+  const float rep = p.repetition ? p.repetition[i] : 1.f, less = 1.f / rep;
+  const float pres = p.presence ? p.presence[i] : 0.f, freq = p.frequency ? p.frequency[i] : 0.f;
+  uint32_t held[2] = {}, drafted[2] = {};
+  float add[2][8] = {};
+  auto added = [&](uint32_t n, int v) {
+    const float bias = s_biased[v >> 5] >> (v & 31) & 1u ? s_bias[v] : 0.f;
+    const uint32_t told = n & ~kPrompt;
+    return told ? bias - (freq * static_cast<float>(told) + pres) : bias;
+  };
+  if constexpr (kSparse) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int byte = tid + e * kThreads;
+      touched[e] = reinterpret_cast<const uint8_t*>(s_touched)[byte];
+      drafted[e] = reinterpret_cast<const uint8_t*>(s_drafted)[byte];
+      if (!touched[e]) continue;
+#pragma unroll
+      for (int b = 0; b < 8; ++b) {
+        const uint32_t n = s_n[at[e] + b];
+        if (n) held[e] |= 1u << b;
+        add[e][b] = added(n, at[e] + b);
       }
     }
   }
+  if (in_place) {
+    read(r0, 0, mask0, x0);
+    read(r0, 1, mask1, x1);
+  }
+  auto finish = [&](int r, int e, uint32_t mask, Unit<T> x) {
+    if (!needed(e, mask)) return;
+    if constexpr (kSparse) {
+      if (__any((touched[e] & mask) != 0)) {
+        float z[8];
+        widen<T>(x, z);
+#pragma unroll
+        for (int b = 0; b < 8; ++b) {
+          if (held[e] >> b & 1u) z[b] *= z[b] > 0.f ? less : rep;
+          z[b] += add[e][b];
+        }
+        Unit<T> y = replaced<T>(x, z, touched[e]);
+        for (uint32_t bits = drafted[e] & mask; bits; bits &= bits - 1) {
+          const int b = __builtin_ctz(bits), v = at[e] + b;
+          uint32_t n = s_n[v];
+          for (int j = 0; j < r; ++j)
+            if (load_invariant(draft + j) == static_cast<int32_t>(v0 + v)) {
+              if (end + 1 + j < answered) n |= kPrompt;
+              else ++n;
+            }
+          float one = take<T>(x, b);
+          if (n) one *= one > 0.f ? less : rep;
+          y = give<T>(y, b, one + added(n, v));
+        }
+        x = y;
+      }
+    }
+    if (mask != 0xFFu) x = masked<T>(x, mask);
+    store_unit(static_cast<T*>(p.out) + ((row0 + r) * p.V + v0) + at[e], x, size - at[e]);
+  };
+  for (int r = r0; r < r1; ++r) {
+    const uint32_t mask0nn = read_mask(r + 2, 0), mask1nn = read_mask(r + 2, 1);
+    const Unit<T> now0 = x0, now1 = x1;
+    if (r + 1 < r1) {
+      read(r + 1, 0, mask0n, x0);
+      read(r + 1, 1, mask1n, x1);
+    }
+    finish(r, 0, mask0, now0);
+    finish(r, 1, mask1, now1);
+    mask0 = mask0n;
+    mask1 = mask1n;
+    mask0n = mask0nn;
+    mask1n = mask1nn;
+  }
+}
+
+template <int kDtype>
+void launch_dtype(const LogitsArgs& a, bool sparse, uint32_t blocks, hipStream_t stream) {
+  if (sparse) logits_kernel<kDtype, true><<<blocks, kThreads, 0, stream>>>(a);
+  else logits_kernel<kDtype, false><<<blocks, kThreads, 0, stream>>>(a);
 }
 
 }  // namespace
 
 hipError_t launch_logits(const LogitsLaunch& p, hipStream_t stream) {
-  LogitsArgs a{p, 0, (static_cast<int64_t>(p.V) + kChunk - 1) / kChunk};
-  return launch_blocks(p.B * a.chunks, kThreads, [&](int64_t at, uint32_t n) {
+  const bool sparse = p.repetition || p.presence || p.frequency || p.n_bias > 0;
+  const int64_t rows = static_cast<int64_t>(p.B) * (p.k + 1);
+  if (p.out == p.logits && !sparse && !p.mask) return hipSuccess;
+  LogitsArgs a{};
+  a.p = p;
+  a.checks = p.mask ? (rows + kThreads / 64 - 1) / (kThreads / 64) : 0;
+  a.chunks = (static_cast<int64_t>(p.V) + kChunk - 1) / kChunk;
+  // the slots go to several workgroups where there would be few otherwise
+  const int64_t items = p.B * a.chunks, wanted = (1024 + items - 1) / items;
+  a.shares = static_cast<int32_t>(wanted < p.k + 1 ? wanted : p.k + 1);
+  a.slots = (p.k + a.shares) / a.shares;
+  a.shares = (p.k + a.slots) / a.slots;
+  return launch_blocks(a.checks + items * a.shares, kThreads, [&](int64_t at, uint32_t n) {
     a.base = at;
-    if (p.dtype == 0) logits_kernel<0><<<n, kThreads, 0, stream>>>(a);
-    else if (p.dtype == 1) logits_kernel<1><<<n, kThreads, 0, stream>>>(a);
-    else logits_kernel<2><<<n, kThreads, 0, stream>>>(a);
+    if (p.dtype == 0) launch_dtype<0>(a, sparse, n, stream);
+    else if (p.dtype == 1) launch_dtype<1>(a, sparse, n, stream);
+    else launch_dtype<2>(a, sparse, n, stream);
   });
 }
 
