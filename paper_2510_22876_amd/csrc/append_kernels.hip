@@ -5,11 +5,17 @@
 //   (a, b) -> (a cos t - b sin t, b cos t + a sin t)   per rotated pair,
 //   t = position * inv_freq_j, position = entries before the window + r (I2)
 //
-// A workgroup takes one token and a share of its heads; a group of lanes
-// (8 elements a lane) takes a head.  Everything is fp32 from the load to one
-// rounding at the store.  The angle is formed in revolutions in fp64: at a
-// position of 2^24 an fp32 product would be off by up to half a radian.
+// A workgroup takes one token, or a share of its heads where there are few
+// tokens; a group of lanes (8 elements a lane) takes a head after the other.
+// A lane meets the same elements of every head, so it keeps their weights,
+// cosines and sines in registers; the other half of a pair comes through LDS,
+// within the wave.  The next head is read while one is worked on, the first
+// before anything else.  Everything is fp32 from the load to one rounding at
+// the store.  The angle is formed in revolutions in fp64: at a position of
+// 2^24 an fp32 product would be off by up to half a radian.
 #include "forward_common.h"
+
+#include <type_traits>
 
 namespace specdec {
 namespace {
@@ -22,22 +28,50 @@ struct AppendArgs {
   int64_t base;           // first workgroup of this launch
   uint32_t shares;        // workgroups a token
   uint32_t lanes;         // lanes a head (a power of two)
+  float per_element;      // 1 / D
 };
+
+// The sum over a group of up to 32 lanes, in all of them: DPP moves within 16
+// lanes (neighbours, pairs, mirrored eights and sixteens), where a shuffle
+// through LDS a step would wait for each.
+__device__ __forceinline__ float group_sum(float x, uint32_t lanes) {
+  auto moved = [](float v, auto how) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), decltype(how)::value, 0xF, 0xF, true));
+  };
+  if (lanes >= 2) x += moved(x, std::integral_constant<int, 0xB1>{});    // quad_perm 1 0 3 2
+  if (lanes >= 4) x += moved(x, std::integral_constant<int, 0x4E>{});    // quad_perm 2 3 0 1
+  if (lanes >= 8) x += moved(x, std::integral_constant<int, 0x141>{});   // row_half_mirror
+  if (lanes >= 16) x += moved(x, std::integral_constant<int, 0x140>{});  // row_mirror
+  if (lanes >= 32) x += __shfl_xor(x, 16);
+  return x;
+}
 
 template <int kDtype>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   typedef typename Element<kDtype>::type T;
   __shared__ float s_cos[kMaxHalf], s_sin[kMaxHalf];
-  __shared__ float s_row[kThreads * 8];
+  __shared__ __align__(16) float s_row[kThreads * 8];
   const AppendLaunch& p = a.p;
   const CacheView& c = p.cache;
   const int64_t block = a.base + blockIdx.x;
   const int token = static_cast<int>(block / a.shares), share = static_cast<int>(block % a.shares);
   const int i = token / p.T, r = token % p.T, tid = threadIdx.x;
+  const int groups = kThreads / a.lanes, group = tid / a.lanes, d0 = tid % a.lanes * 8;
+  const int D = c.D, heads = p.Hq + 2 * c.H, step = groups * a.shares;
+  const bool live = d0 < D;
+  const T* x0 = static_cast<const T*>(p.qkv) + static_cast<int64_t>(token) * heads * D + d0;
+  int h = share * groups + group;
+  float next[8] = {};
+  if (live && h < heads) load_elements(x0 + static_cast<int64_t>(h) * D, next);
+  float gq[8], gk[8];
+  if (p.q_norm && live) load_elements(static_cast<const T*>(p.q_norm) + d0, gq);
+  if (p.k_norm && live) load_elements(static_cast<const T*>(p.k_norm) + d0, gk);
+
   const int32_t n = entries_before(c, i, p.T);
   bool ok = n >= 0;
   if (ok && c.table) {   // every page that the window's entries lie in
-    for (int64_t q = n / c.cap; q <= (n + p.T - 1) / c.cap; ++q) {
+    const uint32_t P = static_cast<uint32_t>(c.cap);
+    for (uint32_t q = static_cast<uint32_t>(n) / P; q <= static_cast<uint32_t>(n + p.T - 1) / P; ++q) {
       const int32_t id = c.table[i * c.table_stride + q];
       ok = ok && id >= 0 && id < c.rows;
     }
@@ -46,58 +80,78 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     if (r == 0 && share == 0 && tid == 0 && p.dev_status) atomicOr(p.dev_status, c.table ? kBadSlot : kBadPadIn);
     return;
   }
-  for (int j = tid; j < p.half; j += kThreads) {
-    const double turns = static_cast<double>(n + r) * static_cast<double>(p.inv_freq[j]) * 0.15915494309189535;
-    sincospif(2.f * static_cast<float>(turns - __builtin_rint(turns)), &s_sin[j], &s_cos[j]);
+  if (tid < p.half) {
+    const double turns = static_cast<double>(n + r) * static_cast<double>(p.inv_freq[tid]) * 0.15915494309189535;
+    sincospif(2.f * static_cast<float>(turns - __builtin_rint(turns)), &s_sin[tid], &s_cos[tid]);
   }
   __syncthreads();
-  const int groups = kThreads / a.lanes, group = tid / a.lanes, lane = tid % a.lanes;
-  const int D = c.D, heads = p.Hq + 2 * c.H, d0 = lane * 8;
-  const T* x0 = static_cast<const T*>(p.qkv) + static_cast<int64_t>(token) * heads * D;
+  // x = x * cs + partner * sn; elements that are not rotated have 1 and 0
+  float cs[8], sn[8];
+  bool turns = false;   // any of the lane's
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int d = d0 + e;
+    cs[e] = 1.f;
+    sn[e] = 0.f;
+    if (d < 2 * p.half) {
+      const bool second = p.adjacent ? (e & 1) != 0 : d >= p.half;
+      const int j = p.adjacent ? d >> 1 : second ? d - p.half : d;
+      cs[e] = s_cos[j];
+      sn[e] = second ? s_sin[j] : -s_sin[j];
+      turns = true;
+    }
+  }
   const int64_t entry = entry_offset(c, i, n, p.T, n + r);
-  for (int first = share * groups; first < heads; first += groups * a.shares) {   // the same count for every group
-    const int h = first + group;
-    const bool live = h < heads && d0 < D, turned = h < p.Hq + c.H;
-    float x[8] = {};
-    if (live) load_elements(x0 + static_cast<int64_t>(h) * D + d0, x);
-    const T* w = static_cast<const T*>(h < p.Hq ? p.q_norm : p.k_norm);
-    if (w && turned) {
+  float* row = s_row + group * a.lanes * 8;
+  while (h - group < heads) {   // the same count for every group of the workgroup
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = next[e];
+    const int at = h;
+    h += step;
+    if (live && h < heads) load_elements(x0 + static_cast<int64_t>(h) * D, next);
+    const bool query = at < p.Hq, key = !query && at < p.Hq + c.H;
+    if (query ? p.q_norm != nullptr : key && p.k_norm) {
       float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum += x[e] * x[e];
-      for (uint32_t m = 1; m < a.lanes; m <<= 1) sum += __shfl_xor(sum, m);
-      const float inv = 1.0f / __builtin_sqrtf(sum / static_cast<float>(D) + p.eps);
-      if (live) {
-        float g[8];
-        load_elements(w + d0, g);
+      sum = group_sum(sum, a.lanes);
+      const float inv = __builtin_amdgcn_rsqf(sum * a.per_element + p.eps);   // about 1 ulp
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * g[e];
-      }
+      for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * (query ? gq[e] : gk[e]);
     }
-    float* row = s_row + group * a.lanes * 8;
-    if (live && turned)
+    if (p.adjacent) {
+      if (query || key) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) row[d0 + e] = x[e];
-    __syncthreads();
-    if (live && turned) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int d = d0 + e;
-        if (d >= 2 * p.half) continue;
-        const int j = p.adjacent ? d >> 1 : d < p.half ? d : d - p.half;
-        const bool second = p.adjacent ? (d & 1) != 0 : d >= p.half;
-        const float y = row[p.adjacent ? d ^ 1 : second ? d - p.half : d + p.half];
-        x[e] = second ? x[e] * s_cos[j] + y * s_sin[j] : x[e] * s_cos[j] - y * s_sin[j];
+        for (int e = 0; e < 8; e += 2) {
+          const float y = x[e], z = x[e + 1];
+          x[e] = y * cs[e] + z * sn[e];
+          x[e + 1] = z * cs[e + 1] + y * sn[e + 1];
+        }
       }
+    } else if (p.half > 0) {
+      // the group's lanes lie in one wave: its LDS accesses keep their order
+      if (live && (query || key)) {
+        *reinterpret_cast<f32x4*>(row + d0) = f32x4{x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<f32x4*>(row + d0 + 4) = f32x4{x[4], x[5], x[6], x[7]};
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (live && turns && (query || key)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int d = d0 + e, other = d >= 2 * p.half ? d : d < p.half ? d + p.half : d - p.half;
+          x[e] = x[e] * cs[e] + row[other] * sn[e];
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    __syncthreads();
-    if (!live) continue;
+    if (!live || at >= heads) continue;
     __bf16* to;
-    if (h < p.Hq) {
-      to = static_cast<__bf16*>(p.q_out) + (static_cast<int64_t>(token) * p.Hq + h) * D;
+    if (query) {
+      to = static_cast<__bf16*>(p.q_out) + (static_cast<int64_t>(token) * p.Hq + at) * D;
     } else {
-      const int g = h - p.Hq;
-      to = static_cast<__bf16*>(g < c.H ? c.k : c.v) + entry + static_cast<int64_t>(g < c.H ? g : g - c.H) * c.cap * D;
+      const int g = at - p.Hq;
+      to = static_cast<__bf16*>(key ? c.k : c.v) + entry + static_cast<int64_t>(key ? g : g - c.H) * c.cap * D;
     }
     store_elements(to + d0, x);
   }
@@ -106,10 +160,12 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
 }  // namespace
 
 hipError_t launch_append(const AppendLaunch& p, hipStream_t stream) {
-  AppendArgs a{p, 0, 1, 1};
+  AppendArgs a{p, 0, 1, 1, 1.f / static_cast<float>(p.cache.D)};
   while (a.lanes * 8 < static_cast<uint32_t>(p.cache.D)) a.lanes *= 2;
   const uint32_t groups = kThreads / a.lanes, heads = static_cast<uint32_t>(p.Hq + 2 * p.cache.H);
-  a.shares = (heads + groups - 1) / groups;
+  // few tokens: the heads go to several workgroups, so that the call waits for fewer heads in turn
+  const int64_t tokens = static_cast<int64_t>(p.B) * p.T, wanted = (1024 + tokens - 1) / tokens, most = (heads + groups - 1) / groups;
+  a.shares = static_cast<uint32_t>(wanted < most ? wanted : most);
   return launch_blocks(static_cast<int64_t>(p.B) * p.T * a.shares, kThreads, [&](int64_t at, uint32_t n) {
     a.base = at;
     if (p.dtype == 0) append_kernel<0><<<n, kThreads, 0, stream>>>(a);
