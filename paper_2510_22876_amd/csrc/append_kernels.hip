@@ -67,23 +67,35 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   if (p.q_norm && live) load_elements(static_cast<const T*>(p.q_norm) + d0, gq);
   if (p.k_norm && live) load_elements(static_cast<const T*>(p.k_norm) + d0, gk);
 
+  // Where the token's entry lies.  The pages are looked up here and judged
+  // after the angles: one wait for memory less in a call of a single token.
   const int32_t n = entries_before(c, i, p.T);
-  bool ok = n >= 0;
-  if (ok && c.table) {   // every page that the window's entries lie in
-    const uint32_t P = static_cast<uint32_t>(c.cap);
-    for (uint32_t q = static_cast<uint32_t>(n) / P; q <= static_cast<uint32_t>(n + p.T - 1) / P; ++q) {
-      const int32_t id = c.table[i * c.table_stride + q];
-      ok = ok && id >= 0 && id < c.rows;
-    }
-  }
-  if (!ok) {
-    if (r == 0 && share == 0 && tid == 0 && p.dev_status) atomicOr(p.dev_status, c.table ? kBadSlot : kBadPadIn);
-    return;
+  const int32_t* table = c.table + i * c.table_stride;
+  const uint32_t P = static_cast<uint32_t>(c.cap);
+  int32_t page = 0, first = 0, last = 0;
+  if (n >= 0 && c.table) {
+    page = load_invariant(table + static_cast<uint32_t>(n + r) / P);
+    first = load_invariant(table + static_cast<uint32_t>(n) / P);
+    last = load_invariant(table + static_cast<uint32_t>(n + p.T - 1) / P);
   }
   if (tid < p.half) {
     const double turns = static_cast<double>(n + r) * static_cast<double>(p.inv_freq[tid]) * 0.15915494309189535;
     sincospif(2.f * static_cast<float>(turns - __builtin_rint(turns)), &s_sin[tid], &s_cos[tid]);
   }
+  // every page that the window's entries lie in has to be one of the pool's
+  auto outside = [&](int32_t id) { return id < 0 || id >= c.rows; };
+  bool bad = n < 0;
+  if (!bad && c.table) {
+    bad = outside(first) || outside(last);
+    for (uint32_t q = static_cast<uint32_t>(n) / P + 1; q < static_cast<uint32_t>(n + p.T - 1) / P; ++q)
+      bad = bad || outside(load_invariant(table + q));
+  }
+  if (bad) {
+    if (r == 0 && share == 0 && tid == 0 && p.dev_status) atomicOr(p.dev_status, c.table ? kBadSlot : kBadPadIn);
+    return;
+  }
+  const int64_t entry = c.table ? page * c.row_stride + static_cast<int64_t>(static_cast<uint32_t>(n + r) % P) * D
+                                : i * c.row_stride + (static_cast<int64_t>(c.width) - p.T + r) * D;
   __syncthreads();
   // x = x * cs + partner * sn; elements that are not rotated have 1 and 0
   float cs[8], sn[8];
@@ -101,7 +113,6 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
       turns = true;
     }
   }
-  const int64_t entry = entry_offset(c, i, n, p.T, n + r);
   float* row = s_row + group * a.lanes * 8;
   while (h - group < heads) {   // the same count for every group of the workgroup
     float x[8];

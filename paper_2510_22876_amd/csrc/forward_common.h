@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "span_copy.h"
 #include "specdec_internal.h"
 
 namespace specdec {
@@ -56,26 +57,11 @@ hipError_t launch_blocks(int64_t blocks, int threads, F&& launch) {
 // or length is out of range.
 __device__ __forceinline__ int32_t entries_before(const CacheView& c, int32_t i, int32_t T) {
   if (c.table) {
-    const int32_t n = c.lens[i];
+    const int32_t n = load_invariant(c.lens + i);
     return n < 0 || n > c.width - T ? -1 : n;
   }
-  const int32_t pad = c.lens[i], L = c.width - T;
+  const int32_t pad = load_invariant(c.lens + i), L = c.width - T;
   return pad < 0 || pad > L ? -1 : L - pad;
-}
-
-// Element offset of entry j of sequence i, head 0, within one (layer, K/V)
-// slab, or -1 where the page that holds it is outside the pool.  The
-// left-padded batch is the case without a table: row i, column pad + j.
-__device__ __forceinline__ int64_t entry_offset(const CacheView& c, int32_t i, int32_t n, int32_t T, int32_t j) {
-  int64_t row = i, col;
-  if (c.table) {
-    row = c.table[i * c.table_stride + j / c.cap];
-    if (row < 0 || row >= c.rows) return -1;
-    col = j % c.cap;
-  } else {
-    col = static_cast<int64_t>(c.width) - T - n + j;
-  }
-  return row * c.row_stride + col * c.D;
 }
 
 }  // namespace specdec
