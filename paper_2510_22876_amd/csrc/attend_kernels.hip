@@ -649,7 +649,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, uin
 // (0: pairs are not cut).
 struct Plan {
   int tiles;
-  int64_t groups, items, pieces, even_pieces;
+  int64_t groups, items, pieces, even_pieces, slots;
 };
 Plan plan_of(int64_t B, int64_t T, int64_t Hq, int64_t H, int64_t D, int64_t max_len) {
   constexpr int64_t kCus = 256;
@@ -672,7 +672,9 @@ Plan plan_of(int64_t B, int64_t T, int64_t Hq, int64_t H, int64_t D, int64_t max
   auto share = [&](int64_t n) { return p.groups >= n / 8 ? 8 : n / p.groups; };
   p.pieces = !cut ? 0 : share(pairs > kCus / 2 ? kCus * 3 / 2 : kCus * 2);
   p.even_pieces = !cut ? 0 : share(p.groups > 1 ? 2 * kCus : kCus);
-  p.items = pairs + p.pieces;
+  const int64_t bound = p.pieces > p.even_pieces ? p.pieces : p.even_pieces;   // find_piece's bounds
+  p.items = pairs + bound;
+  p.slots = 2 * bound;
   return p;
 }
 
@@ -690,7 +692,7 @@ void launch_tiles(const AttendArgs& a, bool paged, uint32_t blocks, hipStream_t 
 
 int64_t attend_workspace(int64_t B, int64_t T, int64_t Hq, int64_t H, int64_t D, int64_t max_len) {
   const Plan p = plan_of(B, T, Hq, H, D, max_len);
-  return (8 * B + 255) / 256 * 256 + 2 * p.pieces * T * (Hq / H) * (D * 4 + 8) + 256;
+  return (8 * B + 255) / 256 * 256 + p.slots * T * (Hq / H) * (D * 4 + 8) + 256;
 }
 
 hipError_t launch_attend(const AttendLaunch& p, hipStream_t stream) {
@@ -713,7 +715,7 @@ hipError_t launch_attend(const AttendLaunch& p, hipStream_t stream) {
   a.dev_status = p.dev_status;
   a.plan = static_cast<int2*>(p.workspace);
   a.part = reinterpret_cast<float*>(static_cast<char*>(p.workspace) + (8 * static_cast<int64_t>(p.B) + 255) / 256 * 256);
-  a.stat = reinterpret_cast<float2*>(a.part + 2 * plan.pieces * a.M * c.D);
+  a.stat = reinterpret_cast<float2*>(a.part + plan.slots * a.M * c.D);
   const bool paged = c.table && c.cap < c.width;
   const int64_t blocks = (plan.items + 7) / 8 * 8 * plan.groups;
   if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;

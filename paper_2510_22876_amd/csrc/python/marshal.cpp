@@ -161,12 +161,13 @@ void* stream_of(PyObject* o) {
   return s;
 }
 
-// The kernels run on the current device.
-void on_current_device(const at::Tensor& t) {
+// The kernels run on the current device: every tensor has to lie there.
+void on_current_device(std::initializer_list<PyObject*> tensors) {
   PyObject* dev = PyObject_CallNoArgs(get_device);
   const long d = dev ? PyLong_AsLong(dev) : -1;
   Py_XDECREF(dev);
-  need(d >= 0 && t.is_cuda() && t.get_device() == d);
+  need(d >= 0);
+  for (PyObject* o : tensors) need(o == Py_None || tensor(o).get_device() == d);
 }
 
 // Runs the library call without the interpreter lock, as ctypes does.
@@ -420,7 +421,6 @@ struct Append {
     dtype = type == at::kFloat ? SPECDEC_F32 : type == at::kBFloat16 ? SPECDEC_BF16 : SPECDEC_F16;
     need((dtype != SPECDEC_F16 || type == at::kHalf) && t.dim() == 4 && t.is_cuda() && t.is_contiguous());
     for (int d : {0, 1, 2, 3}) need(t.size(d) <= INT32_MAX);
-    on_current_device(t);
     kv = cache(kv_);
     B = static_cast<int32_t>(t.size(0));
     T = static_cast<int32_t>(t.size(1));
@@ -448,6 +448,7 @@ struct Append {
 PyObject* append_window(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 13, [&] {
     const Append p(a[0], a[1], a[5], a + 6);
+    on_current_device({a[0], a[1], a[4], a[5], a[6], a[7], a[8], a[11]});
     need(p.kv.B == p.B);
     const int32_t layer = integer(a[2]), W_in = integer(a[3]), *pad_in = ints(a[4], {p.B});
     uint32_t* dev = status(a[11]);
@@ -464,6 +465,7 @@ PyObject* append_window(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* append_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 13, [&] {
     const Append p(a[0], a[1], a[5], a + 6);
+    on_current_device({a[0], a[1], a[3], a[4], a[5], a[6], a[7], a[8], a[11]});
     int64_t table_stride = 0;
     const int32_t layer = integer(a[2]), *table = rows<int32_t>(a[3], at::kInt, p.B, &table_stride), *lens = ints(a[4], {p.B});
     uint32_t* dev = status(a[11]);
@@ -487,7 +489,6 @@ struct Attend {
     const at::Tensor& t = tensor(q_);
     need(t.dim() == 4);
     for (int d : {0, 1, 2, 3}) need(t.size(d) <= INT32_MAX);
-    on_current_device(t);
     kv = cache(kv_);
     need(t.size(3) == kv.D);
     B = static_cast<int32_t>(t.size(0));
@@ -510,6 +511,7 @@ PyObject* attend_window(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 10, [&] {
     const int32_t layer = integer(a[2]), W_in = integer(a[3]);
     const Attend p(a[0], a[1], a[5], a[6], a[7], W_in);
+    on_current_device({a[0], a[1], a[4], a[5], a[6], a[8]});
     need(p.kv.B == p.B);
     const int32_t* pad_in = ints(a[4], {p.B});
     uint32_t* dev = status(a[8]);
@@ -525,6 +527,7 @@ PyObject* attend_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 11, [&] {
     const int32_t layer = integer(a[2]), max_len = integer(a[5]);
     const Attend p(a[0], a[1], a[6], a[7], a[8], max_len);
+    on_current_device({a[0], a[1], a[3], a[4], a[6], a[7], a[9]});
     int64_t table_stride = 0;
     const int32_t *table = rows<int32_t>(a[3], at::kInt, p.B, &table_stride), *lens = ints(a[4], {p.B});
     uint32_t* dev = status(a[9]);
@@ -542,7 +545,7 @@ PyObject* process_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 16, [&] {
     const Logits l = logits_of(a[0]);
     const int64_t B = l.B;
-    on_current_device(tensor(a[0]));
+    on_current_device({a[0], a[1], a[2], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12], a[13], a[14]});
     void* out = dense<void>(a[1], l.type, {B, l.k + 1, l.V});
     int64_t s_stride = 0, n_bias = 0, words = 0;
     const int32_t* s = a[2] != Py_None ? rows<int32_t>(a[2], at::kInt, B, &s_stride) : nullptr;

@@ -654,17 +654,19 @@ def specdec_varlen_rollback(src, dst, cu_in, n_acc, k: int, max_len: int, cu_out
                                        _stream(stream)))
 
 
-def _on_current_device(name, t):
-    """The kernels run on the current device."""
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+def _on_current_device(**tensors):
+    """The kernels run on the current device: every tensor has to lie there."""
+    for name, t in tensors.items():
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
 
 
 def _check_append(qkv, kv, q_out, inv_freq, q_norm, k_norm, dev_status):
     """The arguments that both appends share: (B, T, Hq, descriptor of the cache)."""
     if qkv.dim() != 4 or qkv.dtype not in DTYPE_OF or not qkv.is_cuda or not qkv.is_contiguous():
         raise ValueError("qkv must be a contiguous device tensor [B][T][Hq+2H][D] of float32/bfloat16/float16")
-    _on_current_device("qkv", qkv)
+    _on_current_device(qkv=qkv, cache=kv, q_out=q_out, inv_freq=inv_freq, q_norm=q_norm, k_norm=k_norm,
+                       dev_status=dev_status)
     d = kv_desc(kv)
     B, T, heads, D = qkv.shape
     Hq = heads - 2 * d.H
@@ -691,6 +693,7 @@ def specdec_append_window(qkv, kv, layer: int, W_in: int, pad_in, q_out, inv_fre
     B, T, Hq, d = _check_append(qkv, kv, q_out, inv_freq, q_norm, k_norm, dev_status)
     if d.B != B:
         raise ValueError("cache rows differ from qkv's")
+    _on_current_device(pad_in=pad_in)
     _req("pad_in", pad_in, (B,), torch.int32)
     _check(lib.specdec_append_window(_p(qkv), DTYPE_OF[qkv.dtype], T, Hq, _p(q_norm), _p(k_norm), float(eps),
                                      _p(inv_freq), inv_freq.numel() if inv_freq is not None else 0, 1 if adjacent else 0,
@@ -709,6 +712,7 @@ def specdec_append_paged(qkv, pool, layer: int, table, lens, q_out, inv_freq=Non
         if r is not NotImplemented:
             return _check(r)
     B, T, Hq, d = _check_append(qkv, pool, q_out, inv_freq, q_norm, k_norm, dev_status)
+    _on_current_device(table=table, lens=lens)
     _req("table", table, (B, table.shape[1]), torch.int32)
     _req("lens", lens, (B,), torch.int32)
     _check(lib.specdec_append_paged(_p(qkv), DTYPE_OF[qkv.dtype], B, T, Hq, _p(q_norm), _p(k_norm), float(eps),
@@ -737,7 +741,7 @@ def _check_attend(q, kv, out, workspace, max_len, dev_status):
     if D != d.D:
         raise ValueError("q's head size differs from the cache's")
     _req("q", q, (B, T, Hq, D), torch.bfloat16)
-    _on_current_device("q", q)
+    _on_current_device(q=q, cache=kv, out=out, workspace=workspace, dev_status=dev_status)
     _req("out", out, (B, T, Hq, D), torch.bfloat16)
     _req("dev_status", dev_status, (1,), torch.int32, optional=True)
     nb = workspace.numel() * workspace.element_size()
@@ -758,6 +762,7 @@ def specdec_attend_window(q, kv, layer: int, W_in: int, pad_in, out, workspace, 
     B, T, Hq, d, nb = _check_attend(q, kv, out, workspace, W_in, dev_status)
     if d.B != B:
         raise ValueError("cache rows differ from q's")
+    _on_current_device(pad_in=pad_in)
     _req("pad_in", pad_in, (B,), torch.int32)
     _check(lib.specdec_attend_window(_p(q), T, Hq, d.D ** -0.5 if scale is None else float(scale), ctypes.byref(d), layer,
                                      W_in, _p(pad_in), _p(out), _p(workspace), nb, _p(dev_status), _stream(stream)))
@@ -772,6 +777,7 @@ def specdec_attend_paged(q, pool, layer: int, table, lens, max_len: int, out, wo
         if r is not NotImplemented:
             return _check(r)
     B, T, Hq, d, nb = _check_attend(q, pool, out, workspace, max_len, dev_status)
+    _on_current_device(table=table, lens=lens)
     _req("table", table, (B, table.shape[1]), torch.int32)
     _req("lens", lens, (B,), torch.int32)
     _check(lib.specdec_attend_paged(_p(q), B, T, Hq, d.D ** -0.5 if scale is None else float(scale), ctypes.byref(d),
@@ -794,7 +800,9 @@ def specdec_process_logits(logits, out, s=None, width: int = 0, draft=None, begi
             return _check(r)
     if logits.dim() != 3 or logits.dtype not in DTYPE_OF or not logits.is_cuda or not logits.is_contiguous():
         raise ValueError("logits must be a contiguous device tensor [B][k+1][V] of float32/bfloat16/float16")
-    _on_current_device("logits", logits)
+    _on_current_device(logits=logits, out=out, s=s, draft=draft, begin=begin, lens=lens, prompt=prompt,
+                       repetition=repetition, presence=presence, frequency=frequency, bias_ids=bias_ids, bias=bias,
+                       mask=mask, dev_status=dev_status)
     B, kp1, V = logits.shape
     _req("out", out, (B, kp1, V), logits.dtype)
     _req("s", s, (B, s.shape[1] if s is not None else 0), torch.int32, optional=True)

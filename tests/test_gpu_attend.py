@@ -96,6 +96,35 @@ def test_matches_64_bits(sd, name):
     _check(c, q, out)
 
 
+@pytest.mark.parametrize("even", [True, False])
+@pytest.mark.parametrize("layout", [(64, 8, 8, 20, 3300), (14, 2, 65, 3, 1500), (256, 1, 3, 130, 900), (4, 1, 1, 200, 4000)])
+def test_many_pairs_cut(sd, layout, even):
+    """Batches whose pairs are cut, of many queries (several groups of a pair) and of many sequences: every row is
+    answered, and beyond the workspace's bytes nothing is written."""
+    Hq, H, T, B, most = layout
+    D = 64 if Hq != 256 else 128
+    r = np.random.default_rng(4)
+    n = [most if even else int(x) for x in np.maximum(r.integers(0, most + 1, B) * (r.random(B) < 0.4), 1)]
+    n[B // 2] = most
+    c = ref.Cache(n, T, H, D, 0, layers=1, layer=0)
+    kv = torch.randn(c.shape, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+    q = _queries(c, Hq, 2, 2.0)
+    nb = sd.attend_workspace_bytes(B, T, Hq, H, D, c.W_in)
+    space = torch.full((nb + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    out = torch.full(q.shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+    sd.specdec_attend_window(q.cuda(), kv, 0, c.W_in, c.pad, out, space[:nb])
+    torch.cuda.synchronize()
+    assert bool((space[nb:] == 0x5A).all()) and not bool(torch.isnan(out).any())
+    out, c.kv, picked = out.cpu(), kv.cpu(), sorted({0, B // 2, B - 1, int(np.argmin(n))})
+    heads = sorted({0, Hq // 2, Hq - 1})
+    for i in picked:                                      # some heads of some rows: the plain form takes its time
+        k, v = c.entries(i, n[i] + T)
+        for h in heads:
+            kh, vh = k[:, h // (Hq // H)][:, None], v[:, h // (Hq // H)][:, None]
+            want, bound = ref.attend(q[i][:, h:h + 1], kh, vh, n[i], D ** -0.5)
+            ref.check(out[i][:, h:h + 1], want, bound, f"row {i}, head {h}")
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 1.0, 40.0])
 def test_scales_and_large_scores(sd, scale):
     """No weighting at all, inverted, and scores of several thousand, where all the weight falls on one entry."""
