@@ -26,7 +26,6 @@ namespace {
 
 constexpr uint32_t kBadPadIn = 0x1u, kEmptyMask = 0x80u;
 constexpr uint32_t kPrompt = 0x80000000u;   // the token occurs in the prompt; the low bits count the answered ones
-constexpr int kChunk = 4096, kUnits = kChunk / 8 / kThreads;   // 8 logits a lane, kUnits times
 
 struct LogitsArgs {
   LogitsLaunch p;
@@ -162,10 +161,12 @@ __device__ __forceinline__ Unit<T> masked(Unit<T> u, uint32_t allowed) {
   return u;
 }
 
-template <int kDtype, bool kSparse>   // kSparse: there are penalties or biases
+// kSparse: there are penalties or biases.  kUnits: a lane takes 8 logits that
+// many times, kThreads * 8 apart.
+template <int kDtype, bool kSparse, int kUnits>
 __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
   typedef typename Element<kDtype>::type T;
-  constexpr int kBitWords = kSparse ? kChunk / 32 : 1;
+  constexpr int kChunk = kThreads * 8 * kUnits, kBitWords = kSparse ? kChunk / 32 : 1;
   __shared__ __align__(16) uint32_t s_n[kSparse ? kChunk : 4];
   __shared__ float s_bias[kSparse ? kChunk : 1];
   __shared__ uint32_t s_touched[kBitWords], s_drafted[kBitWords], s_biased[kBitWords];
@@ -199,26 +200,29 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
 
   // A lane's logits are read one slot ahead, and their mask two, which says
   // whether they are needed.
-  static_assert(kUnits == 2, "the units are written out");
   const int64_t row0 = static_cast<int64_t>(i) * (p.k + 1);
-  const int at[2] = {tid * 8, (tid + kThreads) * 8};   // first logit of a lane's units, from v0 on
-  uint32_t touched[2] = {};                            // those that a count, a draft or a bias may change
-  auto read_mask = [&](int r, int e) -> uint32_t {
-    if (!p.mask || at[e] >= size) return 0xFFu;
-    const uint8_t* bits = reinterpret_cast<const uint8_t*>(p.mask + (row0 + (r < r1 ? r : r1 - 1)) * p.mask_stride) + v0 / 8;
-    return bits[at[e] >> 3];
+  uint32_t touched[kUnits] = {};   // those of a lane's logits that a count, a draft or a bias may change
+  auto at = [&](int e) { return (tid + e * kThreads) * 8; };   // the first of them, from v0 on
+  auto read_mask = [&](int r, uint32_t (&to)[kUnits]) {
+#pragma unroll
+    for (int e = 0; e < kUnits; ++e) {
+      to[e] = 0xFFu;
+      if (p.mask && at(e) < size)
+        to[e] = (reinterpret_cast<const uint8_t*>(p.mask + (row0 + (r < r1 ? r : r1 - 1)) * p.mask_stride) + v0 / 8)[tid + e * kThreads];
+    }
   };
-  auto needed = [&](int e, uint32_t mask) { return at[e] < size && !(in_place && mask == 0xFFu && touched[e] == 0); };
-  auto read = [&](int r, int e, uint32_t mask, Unit<T>& x) {
-    if (mask != 0 && needed(e, mask)) x = load_unit(static_cast<const T*>(p.logits) + ((row0 + r) * p.V + v0) + at[e], size - at[e]);
+  auto needed = [&](int e, uint32_t mask) { return at(e) < size && !(in_place && mask == 0xFFu && touched[e] == 0); };
+  auto read = [&](int r, const uint32_t (&mask)[kUnits], Unit<T> (&x)[kUnits]) {
+#pragma unroll
+    for (int e = 0; e < kUnits; ++e)
+      if (mask[e] != 0 && needed(e, mask[e]))
+        x[e] = load_unit(static_cast<const T*>(p.logits) + ((row0 + r) * p.V + v0) + at(e), size - at(e));
   };
-  uint32_t mask0 = read_mask(r0, 0), mask1 = read_mask(r0, 1);
-  uint32_t mask0n = read_mask(r0 + 1, 0), mask1n = read_mask(r0 + 1, 1);
-  Unit<T> x0 = {}, x1 = {};
-  if (!in_place) {   // in place, the counts say which are needed
-    read(r0, 0, mask0, x0);
-    read(r0, 1, mask1, x1);
-  }
+  uint32_t mask[kUnits], mask1[kUnits];
+  read_mask(r0, mask);
+  read_mask(r0 + 1, mask1);
+  Unit<T> x[kUnits] = {};
+  if (!in_place) read(r0, mask, x);   // in place, the counts say whether they are needed
 
   if constexpr (kSparse) {
     const int32_t* ids = p.bias_ids + static_cast<int64_t>(i) * p.n_bias;
@@ -299,12 +303,12 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
       __syncthreads();
     }
   }
-  // What the counts and biases do to a lane's logits: `held` bits say where the
+  // What the counts and biases do to the lane's logits: `held` bits say where the
   // repetition penalty applies, `add` is added.
   const float rep = p.repetition ? p.repetition[i] : 1.f, less = 1.f / rep;
   const float pres = p.presence ? p.presence[i] : 0.f, freq = p.frequency ? p.frequency[i] : 0.f;
-  uint32_t held[2] = {}, drafted[2] = {};
-  float add[2][8] = {};
+  uint32_t held[kUnits] = {}, drafted[kUnits] = {};
+  float add[kUnits][8] = {};
   auto added = [&](uint32_t n, int v) {
     const float bias = s_biased[v >> 5] >> (v & 31) & 1u ? s_bias[v] : 0.f;
     const uint32_t told = n & ~kPrompt;
@@ -312,73 +316,71 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
   };
   if constexpr (kSparse) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int byte = tid + e * kThreads;
-      touched[e] = reinterpret_cast<const uint8_t*>(s_touched)[byte];
-      drafted[e] = reinterpret_cast<const uint8_t*>(s_drafted)[byte];
+    for (int e = 0; e < kUnits; ++e) {
+      touched[e] = reinterpret_cast<const uint8_t*>(s_touched)[tid + e * kThreads];
+      drafted[e] = reinterpret_cast<const uint8_t*>(s_drafted)[tid + e * kThreads];
       if (!touched[e]) continue;
 #pragma unroll
       for (int b = 0; b < 8; ++b) {
-        const uint32_t n = s_n[at[e] + b];
+        const uint32_t n = s_n[at(e) + b];
         if (n) held[e] |= 1u << b;
-        add[e][b] = added(n, at[e] + b);
+        add[e][b] = added(n, at(e) + b);
       }
     }
   }
-  if (in_place) {
-    read(r0, 0, mask0, x0);
-    read(r0, 1, mask1, x1);
-  }
-  auto finish = [&](int r, int e, uint32_t mask, Unit<T> x) {
-    if (!needed(e, mask)) return;
-    if constexpr (kSparse) {
-      if (__any((touched[e] & mask) != 0)) {
-        float z[8];
-        widen<T>(x, z);
-#pragma unroll
-        for (int b = 0; b < 8; ++b) {
-          if (held[e] >> b & 1u) z[b] *= z[b] > 0.f ? less : rep;
-          z[b] += add[e][b];
-        }
-        Unit<T> y = replaced<T>(x, z, touched[e]);
-        for (uint32_t bits = drafted[e] & mask; bits; bits &= bits - 1) {
-          const int b = __builtin_ctz(bits), v = at[e] + b;
-          uint32_t n = s_n[v];
-          for (int j = 0; j < r; ++j)
-            if (load_invariant(draft + j) == static_cast<int32_t>(v0 + v)) {
-              if (end + 1 + j < answered) n |= kPrompt;
-              else ++n;
-            }
-          float one = take<T>(x, b);
-          if (n) one *= one > 0.f ? less : rep;
-          y = give<T>(y, b, one + added(n, v));
-        }
-        x = y;
-      }
-    }
-    if (mask != 0xFFu) x = masked<T>(x, mask);
-    store_unit(static_cast<T*>(p.out) + ((row0 + r) * p.V + v0) + at[e], x, size - at[e]);
-  };
+  if (in_place) read(r0, mask, x);
   for (int r = r0; r < r1; ++r) {
-    const uint32_t mask0nn = read_mask(r + 2, 0), mask1nn = read_mask(r + 2, 1);
-    const Unit<T> now0 = x0, now1 = x1;
-    if (r + 1 < r1) {
-      read(r + 1, 0, mask0n, x0);
-      read(r + 1, 1, mask1n, x1);
+    uint32_t mask2[kUnits];
+    read_mask(r + 2, mask2);
+    Unit<T> now[kUnits];
+#pragma unroll
+    for (int e = 0; e < kUnits; ++e) now[e] = x[e];
+    if (r + 1 < r1) read(r + 1, mask1, x);
+#pragma unroll
+    for (int e = 0; e < kUnits; ++e) {
+      if (!needed(e, mask[e])) continue;
+      Unit<T> y = now[e];
+      if constexpr (kSparse) {
+        if (__any((touched[e] & mask[e]) != 0)) {
+          float z[8];
+          widen<T>(y, z);
+#pragma unroll
+          for (int b = 0; b < 8; ++b) {
+            if (held[e] >> b & 1u) z[b] *= z[b] > 0.f ? less : rep;
+            z[b] += add[e][b];
+          }
+          y = replaced<T>(y, z, touched[e]);
+          for (uint32_t bits = drafted[e] & mask[e]; bits; bits &= bits - 1) {
+            const int b = __builtin_ctz(bits), v = at(e) + b;
+            uint32_t n = s_n[v];
+            for (int j = 0; j < r; ++j)
+              if (load_invariant(draft + j) == static_cast<int32_t>(v0 + v)) {
+                if (end + 1 + j < answered) n |= kPrompt;
+                else ++n;
+              }
+            float one = take<T>(now[e], b);
+            if (n) one *= one > 0.f ? less : rep;
+            y = give<T>(y, b, one + added(n, v));
+          }
+        }
+      }
+      if (mask[e] != 0xFFu) y = masked<T>(y, mask[e]);
+      store_unit(static_cast<T*>(p.out) + ((row0 + r) * p.V + v0) + at(e), y, size - at(e));
     }
-    finish(r, 0, mask0, now0);
-    finish(r, 1, mask1, now1);
-    mask0 = mask0n;
-    mask1 = mask1n;
-    mask0n = mask0nn;
-    mask1n = mask1nn;
+#pragma unroll
+    for (int e = 0; e < kUnits; ++e) {
+      mask[e] = mask1[e];
+      mask1[e] = mask2[e];
+    }
   }
 }
 
 template <int kDtype>
-void launch_dtype(const LogitsArgs& a, bool sparse, uint32_t blocks, hipStream_t stream) {
-  if (sparse) logits_kernel<kDtype, true><<<blocks, kThreads, 0, stream>>>(a);
-  else logits_kernel<kDtype, false><<<blocks, kThreads, 0, stream>>>(a);
+void launch_dtype(const LogitsArgs& a, bool sparse, int units, uint32_t blocks, hipStream_t stream) {
+  if (sparse && units == 1) logits_kernel<kDtype, true, 1><<<blocks, kThreads, 0, stream>>>(a);
+  else if (sparse) logits_kernel<kDtype, true, 2><<<blocks, kThreads, 0, stream>>>(a);
+  else if (units == 1) logits_kernel<kDtype, false, 1><<<blocks, kThreads, 0, stream>>>(a);
+  else logits_kernel<kDtype, false, 2><<<blocks, kThreads, 0, stream>>>(a);
 }
 
 }  // namespace
@@ -390,7 +392,12 @@ hipError_t launch_logits(const LogitsLaunch& p, hipStream_t stream) {
   LogitsArgs a{};
   a.p = p;
   a.checks = p.mask ? (rows + kThreads / 64 - 1) / (kThreads / 64) : 0;
-  a.chunks = (static_cast<int64_t>(p.V) + kChunk - 1) / kChunk;
+  // Two units a lane need fewer set-ups and keep more loads in flight; one
+  // fills the CUs with less (1 x 128256: 7.1 us with two, 5.3 with one; 32 x 8
+  // x 128256 with everything on: 36 and 44).
+  const int units = p.B * ((static_cast<int64_t>(p.V) + 16 * kThreads - 1) / (16 * kThreads)) < 512 ? 1 : 2;
+  const int64_t chunk = 8 * kThreads * units;
+  a.chunks = (p.V + chunk - 1) / chunk;
   // the slots go to several workgroups where there would be few otherwise
   const int64_t items = p.B * a.chunks, wanted = (1024 + items - 1) / items;
   a.shares = static_cast<int32_t>(wanted < p.k + 1 ? wanted : p.k + 1);
@@ -398,9 +405,9 @@ hipError_t launch_logits(const LogitsLaunch& p, hipStream_t stream) {
   a.shares = (p.k + a.slots) / a.slots;
   return launch_blocks(a.checks + items * a.shares, kThreads, [&](int64_t at, uint32_t n) {
     a.base = at;
-    if (p.dtype == 0) launch_dtype<0>(a, sparse, n, stream);
-    else if (p.dtype == 1) launch_dtype<1>(a, sparse, n, stream);
-    else launch_dtype<2>(a, sparse, n, stream);
+    if (p.dtype == 0) launch_dtype<0>(a, sparse, units, n, stream);
+    else if (p.dtype == 1) launch_dtype<1>(a, sparse, units, n, stream);
+    else launch_dtype<2>(a, sparse, units, n, stream);
   });
 }
 
