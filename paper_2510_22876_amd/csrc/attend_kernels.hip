@@ -49,6 +49,7 @@ constexpr int kWaves = 4;
 constexpr int kTile = 32;                 // entries a wave takes at a time
 constexpr int kMaxCutB = 1024;            // sequences that a workgroup scans
 constexpr uint32_t kLeastPiece = 4;       // tiles
+constexpr uint32_t kCus = 256;
 constexpr float kLowest = -3.0e38f;       // the maximum of no score
 constexpr float kSlack = 8.f;             // powers of two that a weight may exceed 1 by
 constexpr float kBadPiece = -1.f;         // a piece's sum of weights: it has met a page outside the pool
@@ -64,8 +65,7 @@ struct AttendArgs {
   int32_t B, T, Hq, G, M; // M = T * G queries share a KV head
   uint32_t groups;        // of 16 * MT queries
   uint32_t items;         // workgroups a group
-  uint32_t pieces;        // pieces that the batch's entries are cut into, about (0: pairs are not cut),
-  uint32_t even_pieces;   // and where the sequences are about equally long
+  uint32_t pieces;        // pieces that the batch's entries are cut into, about (0: pairs are not cut)
   float c2;               // scale * log2(e)
   uint32_t* dev_status;
 };
@@ -164,10 +164,34 @@ struct Piece {
   int32_t slot;
 };
 
-// Finds the workgroup's piece by a scan of the sequences.  With `t` tiles in
-// all, a piece has at most ceil(t / pieces) tiles, rounded up to a multiple of
-// kLeastPiece; a sequence of more has as many equal ones as that takes.  So
-// there are at most pieces + pairs of them, and 2 * pieces of cut pairs.
+// Op over the lanes up to this one, in the last lane over the wave; 0 is op's
+// neutral element.
+template <class Op>
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v, Op op) {
+  auto step = [&](auto how, auto rows) {
+    v = op(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), decltype(how)::value, decltype(rows)::value, 0xF, false)));
+  };
+  using std::integral_constant;
+  step(integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});   // one lane to the right in each 16,
+  step(integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});   // two,
+  step(integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});   // four,
+  step(integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});   // eight;
+  step(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});   // the 16's last lane to the next 16,
+  step(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});   // the lower half's to the upper
+  return v;
+}
+__device__ __forceinline__ uint32_t wave_last(uint32_t v) { return __builtin_amdgcn_readlane(v, 63); }
+
+// Finds the workgroup's piece by a scan of the sequences.  Pieces have at most
+// `most` tiles, a multiple of kLeastPiece; a sequence of more has as many equal
+// ones as that takes.
+// Unequal sequences of `t` tiles in all: most = t / a.pieces, rounded up, so
+// that there are at most a.pieces + pairs pieces, 2 * a.pieces of cut pairs.
+// About equal ones: the pairs get as many pieces each as lets the CU with the
+// most of them end first, a piece counted as kLeastPiece tiles more than it has
+// for what it begins and ends with, and a.pieces pieces at most in all (35 x 4
+// KV heads of 256, window 5, 3762 to 4180 entries: 70 us, where 256 pieces cut
+// by length alone give 140 whole pairs and take 96).
 // False: no piece is left for this workgroup.
 __device__ __forceinline__ bool find_piece(const AttendArgs& a, uint32_t item, bool first, Piece* p) {
   constexpr int kEach = kMaxCutB / kThreads;
@@ -185,12 +209,10 @@ __device__ __forceinline__ bool find_piece(const AttendArgs& a, uint32_t item, b
     top = top > tiles[e] ? top : tiles[e];
     if (first && i < a.B && n[e] < 0 && a.dev_status) atomicOr(a.dev_status, a.c.table ? kBadSlot : kBadPadIn);
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    sum += __shfl_xor(sum, d);
-    const uint32_t other = __shfl_xor(top, d);
-    top = top > other ? top : other;
-  }
+  const auto add = [](uint32_t x, uint32_t y) { return x + y; };
+  const auto larger = [](uint32_t x, uint32_t y) { return x > y ? x : y; };
+  sum = wave_last(wave_scan(sum, add));
+  top = wave_last(wave_scan(top, larger));
   if (lane == 0) {
     s_sum[wave] = sum;
     s_top[wave] = top;
@@ -205,8 +227,19 @@ __device__ __forceinline__ bool find_piece(const AttendArgs& a, uint32_t item, b
   }
   const uint64_t all = static_cast<uint64_t>(sum) * a.c.H;
   const bool even = static_cast<uint64_t>(top) * a.B * 8 <= static_cast<uint64_t>(sum) * 9;
-  const uint32_t wanted = even ? a.even_pieces : a.pieces;
-  const uint32_t most = (static_cast<uint32_t>((all + wanted - 1) / wanted) + kLeastPiece - 1) / kLeastPiece * kLeastPiece;
+  uint32_t most;
+  if (even) {   // a lane a number of pieces, the fewest of the best
+    const uint32_t pairs = static_cast<uint32_t>(a.B * a.c.H), step = 1 + kCus / (64 * pairs), each = (lane + 1) * step;
+    const uint32_t size = ((top + each - 1) / each + kLeastPiece - 1) / kLeastPiece * kLeastPiece;
+    const uint32_t rounds = (pairs * each * a.groups + kCus - 1) / kCus;
+    const uint64_t time = static_cast<uint64_t>(rounds) * (size + kLeastPiece);
+    constexpr uint32_t kNever = (1u << 26) - 1;
+    const uint32_t cost = (each == step || pairs * each <= a.pieces) && time < kNever ? static_cast<uint32_t>(time) : kNever;
+    const uint32_t best = ~wave_last(wave_scan(~(cost << 6 | static_cast<uint32_t>(lane)), larger));
+    most = __builtin_amdgcn_readlane(size, best & 63);
+  } else {
+    most = (static_cast<uint32_t>((all + a.pieces - 1) / a.pieces) + kLeastPiece - 1) / kLeastPiece * kLeastPiece;
+  }
   uint32_t mine[kEach], pieces = 0, cut = 0, at[kEach], cut_at[kEach];
 #pragma unroll
   for (int e = 0; e < kEach; ++e) {
@@ -216,15 +249,7 @@ __device__ __forceinline__ bool find_piece(const AttendArgs& a, uint32_t item, b
     pieces += mine[e];
     cut += mine[e] > 1 ? mine[e] : 0u;
   }
-  uint32_t pieces_to = pieces, cut_to = cut;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t v = __shfl_up(pieces_to, d), w = __shfl_up(cut_to, d);
-    if (lane >= d) {
-      pieces_to += v;
-      cut_to += w;
-    }
-  }
+  const uint32_t pieces_to = wave_scan(pieces, add), cut_to = wave_scan(cut, add);
   if (lane == 63) {
     s_pieces[wave] = pieces_to;
     s_cut[wave] = cut_to;
@@ -649,32 +674,27 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, uin
 // (0: pairs are not cut).
 struct Plan {
   int tiles;
-  int64_t groups, items, pieces, even_pieces, slots;
+  int64_t groups, items, pieces, slots;
 };
 Plan plan_of(int64_t B, int64_t T, int64_t Hq, int64_t H, int64_t D, int64_t max_len) {
-  constexpr int64_t kCus = 256;
   Plan p;
   const int64_t tiles = (T * (Hq / H) + 15) / 16, most = D > 128 ? 2 : 3, pairs = B * H;
   p.groups = (tiles + most - 1) / most;
   p.tiles = static_cast<int>((tiles + p.groups - 1) / p.groups);
-  // A CU alone reads about 50 KB a microsecond, so a pair of 1000 entries of
-  // 512 bytes takes some 13 us uncut; the scan and the second kernel cost 7.
-  // Where the CUs are busy with other pairs a longer one may stay whole
-  // (Vicuna-7B's batch of 8, 256 pairs of at most 1030 entries: 16.1 us whole,
-  // 19.5 cut; 8 pairs of 1001: 13.7 and 11.6).
-  const int64_t bytes = max_len * D * 4;
+  // A workgroup reads about 50 KB a microsecond (smaller heads than 128 do not
+  // make a tile faster), so a pair of 1000 entries of 512 bytes takes some 13
+  // us uncut; the scan and the second kernel cost 7.  Where the CUs are busy
+  // with other pairs a longer one may stay whole (Vicuna-7B's batch of 8, 256
+  // pairs of at most 1030 entries: 16.1 us whole, 19.5 cut; 8 pairs of 1001:
+  // 13.7 and 11.6).
+  const int64_t bytes = max_len * (D > 128 ? D : 128) * 4;
   const bool cut = bytes > (pairs >= kCus / 2 ? 768 : 320) * 1024 && B <= kMaxCutB && pairs <= 4096;
-  // Pieces: of equal sequences a whole number a CU, so that no CU has one more
-  // than the others (one of 150001 entries: 123 us with 256, 137 with 384, 127
-  // with 512); of unequal ones more and smaller (64 of 512 to 8192, 256 pairs:
-  // 104 us with 256, 91 with 384, 98 with 512), and more again where there are
-  // few pairs, whose own number adds to them.
-  auto share = [&](int64_t n) { return p.groups >= n / 8 ? 8 : n / p.groups; };
-  p.pieces = !cut ? 0 : share(pairs > kCus / 2 ? kCus * 3 / 2 : kCus * 2);
-  p.even_pieces = !cut ? 0 : share(p.groups > 1 ? 2 * kCus : kCus);
-  const int64_t bound = p.pieces > p.even_pieces ? p.pieces : p.even_pieces;   // find_piece's bounds
-  p.items = pairs + bound;
-  p.slots = 2 * bound;
+  // Pieces of unequal sequences: 3/2 a CU (64 of 512 to 8192, 256 pairs: 104 us
+  // with 1, 91 with 3/2, 98 with 2), more where few pairs add their number.
+  const int64_t wanted = pairs > kCus / 2 ? kCus * 3 / 2 : kCus * 2;
+  p.pieces = !cut ? 0 : p.groups >= wanted / 8 ? 8 : wanted / p.groups;
+  p.items = pairs + p.pieces;
+  p.slots = 2 * p.pieces;
   return p;
 }
 
@@ -710,7 +730,6 @@ hipError_t launch_attend(const AttendLaunch& p, hipStream_t stream) {
   a.groups = static_cast<uint32_t>(plan.groups);
   a.items = static_cast<uint32_t>(plan.items);
   a.pieces = static_cast<uint32_t>(plan.pieces);
-  a.even_pieces = static_cast<uint32_t>(plan.even_pieces);
   a.c2 = p.scale * 1.4426950408889634f;
   a.dev_status = p.dev_status;
   a.plan = static_cast<int2*>(p.workspace);
