@@ -586,11 +586,11 @@ specdec_status_t specdec_varlen_rollback(const specdec_varlen_t* src, const spec
  *   _paged   pages of a pool cache [L][2][N][H][P][D] (pool->B = N pages of
  *            pool->cap = P entries, any P >= 1): entry j of sequence i lies in
  *            page table[i][j / P] at column j % P; c_i = lens[i] entries are
- *            cached, the window's are entries lens[i] .. lens[i] + T - 1.
- *            N * H * P < 2^32.  EXSpec's pool of whole sequences is the case of one page each
- *            (table = slots, a stride of 1), so that a forward needs no
- *            gather.  After verification lens[i] grows by n_acc[i] + 1:
- *            rejected entries are overwritten by the next window.
+ *            cached, the window's are entries lens[i] .. lens[i] + T - 1;
+ *            N * H * P < 2^32.  EXSpec's pool of whole sequences is the case
+ *            of one page each (table = slots, a stride of 1), so that a
+ *            forward needs no gather.  After verification lens[i] grows by
+ *            n_acc[i] + 1: rejected entries are overwritten by the next window.
  *
  * The head size D is a multiple of 8, at most SPECDEC_MAX_HEAD_D.  Hq query
  * heads share the cache's H heads: Hq is a multiple of H, query head h reads
@@ -607,6 +607,8 @@ specdec_status_t specdec_varlen_rollback(const specdec_varlen_t* src, const spec
  * anything.  Sequences must not share the pages that a call appends to (not
  * checked: the contents of the shared entries are then unspecified); shared
  * pages are read by attention like any others.
+ *
+ * These calls have no timer of specdec_timing_*.
  */
 
 /*
@@ -651,7 +653,8 @@ specdec_status_t specdec_append_paged(const void* qkv, int32_t dtype, int32_t B,
  *   out       bf16 [B][T][Hq][D] out, 16-byte aligned.
  *   workspace specdec_attend_workspace_bytes(B, T, Hq, H, D, max_len) bytes,
  *             16-byte aligned, with max_len = W_in for the batch; it needs no
- *             initialisation.
+ *             initialisation and keeps nothing between calls.  Calls that may
+ *             run at the same time need one each.
  * Scores, the softmax's statistics and the sums are fp32; the weights p are
  * rounded to bf16 for the matrix cores, and their sum is taken of the rounded
  * ones.  The result does not depend on the order in which workgroups run.
@@ -698,12 +701,13 @@ specdec_status_t specdec_attend_paged(const void* q, int32_t B, int32_t T, int32
  *   bias_ids, bias  int32 / float [B][n_bias], n_bias <= SPECDEC_MAX_BIAS.
  *   mask      uint32 [B][k+1][mask_stride], mask_stride >= ceil(V / 32), or
  *             NULL.
- * A sequence without 0 <= begin[i] <= end_i < s_stride is left untouched and
- * flagged SPECDEC_DEV_BAD_PAD_IN.  A slot whose mask allows no token becomes
+ * With a penalty, a sequence without 0 <= begin[i] <= end_i < s_stride is left
+ * untouched and flagged SPECDEC_DEV_BAD_PAD_IN; without one nothing looks at
+ * begin and lens.  A slot whose mask allows no token becomes
  * -inf throughout and is flagged SPECDEC_DEV_EMPTY_MASK: greedy verification
  * then answers token 0, stochastic verification an unspecified one.
- * The arithmetic is fp32 with one rounding to `dtype` at the end.
- * Limits as specdec_verify_greedy.
+ * The arithmetic is fp32 with one rounding to `dtype` at the end; a logit that
+ * none of these changes is copied as it is.  Limits as specdec_verify_greedy.
  */
 specdec_status_t specdec_process_logits(const void* logits, void* out, int32_t dtype, int32_t B, int32_t k, int32_t V,
                                         const int32_t* s, int64_t s_stride, int32_t width, const int32_t* draft,

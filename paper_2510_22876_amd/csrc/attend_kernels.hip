@@ -189,9 +189,9 @@ __device__ __forceinline__ uint32_t wave_last(uint32_t v) { return __builtin_amd
 // that there are at most a.pieces + pairs pieces, 2 * a.pieces of cut pairs.
 // About equal ones: the pairs get as many pieces each as lets the CU with the
 // most of them end first, a piece counted as kLeastPiece tiles more than it has
-// for what it begins and ends with, and a.pieces pieces at most in all (35 x 4
-// KV heads of 256, window 5, 3762 to 4180 entries: 70 us, where 256 pieces cut
-// by length alone give 140 whole pairs and take 96).
+// for what it begins and ends with, and a.pieces pieces at most in all (35 x 2
+// KV heads of 256, window 5, 3762 to 4180 entries: 70 us, where about 256
+// pieces, four a pair, leave 24 CUs with a second one and take 96).
 // False: no piece is left for this workgroup.
 __device__ __forceinline__ bool find_piece(const AttendArgs& a, uint32_t item, bool first, Piece* p) {
   constexpr int kEach = kMaxCutB / kThreads;

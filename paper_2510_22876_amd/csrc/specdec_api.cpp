@@ -1182,7 +1182,7 @@ specdec_status_t check_window(const specdec_kv_t* kv, const char* name, int32_t 
   c->cap = kv->cap;
   c->row_stride = kv->cap * kv->D * kv->H;
   const int64_t slab = c->row_stride * kv->B * 2;
-  c->k = static_cast<char*>(kv->data) + 2 * layer * slab;
+  c->k = static_cast<char*>(kv->data) + 2 * static_cast<int64_t>(layer) * slab;
   c->v = static_cast<char*>(c->k) + slab;
   return SPECDEC_OK;
 }

@@ -125,6 +125,32 @@ def test_many_pairs_cut(sd, layout, even):
             ref.check(out[i][:, h:h + 1], want, bound, f"row {i}, head {h}")
 
 
+@pytest.mark.parametrize("T, G", [(1, 1), (65, 48)])
+@pytest.mark.parametrize("pairs", [(1, 1), (2, 1), (3, 1), (1, 4), (5, 1), (9, 1)])
+def test_few_pairs_cut(sd, pairs, T, G):
+    """One to nine pairs of nearly equal length, cut into as many pieces as their queries leave room for."""
+    B, H = pairs
+    n = [2990 - 7 * i for i in range(B)]
+    c = ref.Cache(n, T, H, 64, 16 if B == 2 else 0, layers=1, layer=0)
+    c.fill(T, torch.Generator().manual_seed(3))
+    kv, q = c.kv.cuda(), _queries(c, G * H, 4, 2.0)
+    nb = sd.attend_workspace_bytes(B, T, G * H, H, 64, c.max_len if c.page else c.W_in)
+    space = torch.full((nb + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    out = torch.full(q.shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+    if c.page:
+        sd.specdec_attend_paged(q.cuda(), kv, 0, c.table, c.lens, c.max_len, out, space[:nb])
+    else:
+        sd.specdec_attend_window(q.cuda(), kv, 0, c.W_in, c.pad, out, space[:nb])
+    torch.cuda.synchronize()
+    assert bool((space[nb:] == 0x5A).all()) and not bool(torch.isnan(out).any())
+    out = out.cpu()
+    for i in {0, B - 1}:
+        k, v = c.entries(i, n[i] + T)
+        for h in sorted({0, G * H - 1}):
+            want, bound = ref.attend(q[i][:, h:h + 1], k[:, h // G][:, None], v[:, h // G][:, None], n[i], 64 ** -0.5)
+            ref.check(out[i][:, h:h + 1], want, bound, f"row {i}, head {h}")
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 1.0, 40.0])
 def test_scales_and_large_scores(sd, scale):
     """No weighting at all, inverted, and scores of several thousand, where all the weight falls on one entry."""
