@@ -63,35 +63,14 @@ template <typename T> struct UnitOf { typedef Words4 type; };
 template <> struct UnitOf<float> { typedef Words8 type; };
 template <typename T> using Unit = typename UnitOf<T>::type;
 
-// The first `count` of them lie within the vocabulary.
 template <typename T>
-__device__ __forceinline__ Unit<T> load_unit(const T* p, int count) {
-  Unit<T> u = {};
-  if (count >= 8) {
-    __builtin_memcpy(&u, p, sizeof(u));
-  } else {
-#pragma unroll
-    for (int e = 0; e < 7; ++e) {
-      if (e >= count) break;
-      if constexpr (sizeof(T) == 4) u[e] = __float_as_uint(p[e]);
-      else u[e >> 1] |= static_cast<uint32_t>(__builtin_bit_cast(uint16_t, p[e])) << (e & 1) * 16;
-    }
-  }
+__device__ __forceinline__ Unit<T> load_unit(const T* p) {
+  Unit<T> u;
+  __builtin_memcpy(&u, p, sizeof(u));
   return u;
 }
 template <typename T>
-__device__ __forceinline__ void store_unit(T* p, Unit<T> u, int count) {
-  if (count >= 8) {
-    __builtin_memcpy(p, &u, sizeof(u));
-  } else {
-#pragma unroll
-    for (int e = 0; e < 7; ++e) {
-      if (e >= count) break;
-      if constexpr (sizeof(T) == 4) p[e] = __uint_as_float(u[e]);
-      else p[e] = __builtin_bit_cast(T, static_cast<uint16_t>(u[e >> 1] >> (e & 1) * 16));
-    }
-  }
-}
+__device__ __forceinline__ void store_unit(T* p, Unit<T> u) { __builtin_memcpy(p, &u, sizeof(u)); }
 
 // Logit e of a unit, and its replacement.
 template <typename T>
@@ -183,18 +162,26 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
   const int64_t chunk = block % a.chunks, v0 = chunk * kChunk, rest = block / a.chunks;
   const int i = static_cast<int>(rest / a.shares), r0 = static_cast<int>(rest % a.shares) * a.slots;
   const int r1 = r0 + a.slots < p.k + 1 ? r0 + a.slots : p.k + 1;
-  const int size = static_cast<int>(p.V - v0 < kChunk ? p.V - v0 : kChunk);
+  const int size = static_cast<int>(p.V - v0 < kChunk ? p.V - v0 : kChunk), whole = size & ~7;   // units of 8 end there
   const bool penal = p.repetition || p.presence || p.frequency;
   int64_t begin = 0, end = p.width, answered = 0;   // columns of the history; the first behind the prompt
   const int32_t* draft = p.draft + static_cast<int64_t>(i) * p.k;
+  float rep = 1.f, pres = 0.f, freq = 0.f;
   if (kSparse && penal) {
-    if (p.begin) begin = load_invariant(p.begin + i);
-    if (p.lens) end = load_invariant(p.lens + i);
+    // read together: what is not given stands for any word that may be read
+    auto word = [&](const void* of) { return load_invariant(of ? static_cast<const int32_t*>(of) + i : p.s); };
+    const int32_t b = word(p.begin), l = word(p.lens), t = word(p.prompt);
+    const int32_t x = word(p.repetition), y = word(p.presence), z = word(p.frequency);
+    begin = p.begin ? b : 0;
+    end = p.lens ? l : p.width;
+    answered = begin + (p.prompt ? t : 0);
+    rep = p.repetition ? __int_as_float(x) : 1.f;
+    pres = p.presence ? __int_as_float(y) : 0.f;
+    freq = p.frequency ? __int_as_float(z) : 0.f;
     if (begin < 0 || begin > end || end >= p.s_stride) {
       if (chunk == 0 && r0 == 0 && tid == 0 && p.dev_status) atomicOr(p.dev_status, kBadPadIn);
       return;
     }
-    answered = begin + (p.prompt ? load_invariant(p.prompt + i) : 0);
   }
   const bool in_place = p.out == p.logits;
 
@@ -207,37 +194,61 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
 #pragma unroll
     for (int e = 0; e < kUnits; ++e) {
       to[e] = 0xFFu;
-      if (p.mask && at(e) < size)
+      if (p.mask && at(e) < whole)
         to[e] = (reinterpret_cast<const uint8_t*>(p.mask + (row0 + (r < r1 ? r : r1 - 1)) * p.mask_stride) + v0 / 8)[tid + e * kThreads];
     }
   };
-  auto needed = [&](int e, uint32_t mask) { return at(e) < size && !(in_place && mask == 0xFFu && touched[e] == 0); };
+  auto needed = [&](int e, uint32_t mask) { return at(e) < whole && !(in_place && mask == 0xFFu && touched[e] == 0); };
   auto read = [&](int r, const uint32_t (&mask)[kUnits], Unit<T> (&x)[kUnits]) {
 #pragma unroll
     for (int e = 0; e < kUnits; ++e)
       if (mask[e] != 0 && needed(e, mask[e]))
-        x[e] = load_unit(static_cast<const T*>(p.logits) + ((row0 + r) * p.V + v0) + at(e), size - at(e));
+        x[e] = load_unit(static_cast<const T*>(p.logits) + ((row0 + r) * p.V + v0) + at(e));
   };
   uint32_t mask[kUnits], mask1[kUnits];
   read_mask(r0, mask);
   read_mask(r0 + 1, mask1);
   Unit<T> x[kUnits] = {};
-  if (!in_place) read(r0, mask, x);   // in place, the counts say whether they are needed
+  // In place, the counts say whether they are needed.  Few logits: at once;
+  // many: behind what the counts need, which is then not waited for longer.
+  constexpr bool kAtOnce = !kSparse || kUnits == 1;
+  if (kAtOnce && !in_place) read(r0, mask, x);
 
   if constexpr (kSparse) {
+    // All that the counts need is read before the first wait, but for the
+    // tokens of a history beyond kAhead * kThreads.
+    constexpr int kBiases = SPECDEC_MAX_BIAS / kThreads, kAhead = 8;
     const int32_t* ids = p.bias_ids + static_cast<int64_t>(i) * p.n_bias;
     const float* bias = p.bias + static_cast<int64_t>(i) * p.n_bias;
+    const int32_t* s = p.s + i * p.s_stride;
+    int32_t early[kAhead], id[kBiases], drafted_token = -1;
+    float bias_of[kBiases];
+#pragma unroll
+    for (int e = 0; e < kBiases; ++e) {
+      const int j = tid + e * kThreads;
+      id[e] = j < p.n_bias ? ids[j] : -1;
+      bias_of[e] = j < p.n_bias ? bias[j] : 0.f;
+    }
+    if (penal) {
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) {
+        const int64_t j = begin + e * kThreads + tid;
+        early[e] = j <= end ? s[j] : -1;
+      }
+      if (tid < r1 - 1) drafted_token = draft[tid];   // (k is below the threads)
+    }
     uint32_t* s_place = reinterpret_cast<uint32_t*>(s_bias);
     auto inside = [&](int32_t token) { return token >= v0 && token < v0 + size; };
     auto mark = [](uint32_t* bits, int v) { atomicOr(&bits[v >> 5], 1u << (v & 31)); };
     for (int j = tid; j < kChunk / 4; j += kThreads) reinterpret_cast<uint4*>(s_n)[j] = uint4{0, 0, 0, 0};
     for (int j = tid; j < kChunk / 32; j += kThreads) s_touched[j] = s_drafted[j] = s_biased[j] = 0;
-    for (int j = tid; j < p.n_bias; j += kThreads)
-      if (inside(ids[j])) s_place[ids[j] - v0] = ~0u;
+#pragma unroll
+    for (int e = 0; e < kBiases; ++e)
+      if (inside(id[e])) s_place[id[e] - v0] = ~0u;
     if (tid == 0) s_again = 0;
     __syncthreads();
+    if (!kAtOnce && !in_place) read(r0, mask, x);
     if (penal) {
-      const int32_t* s = p.s + i * p.s_stride;
       auto count = [&](int64_t j, int32_t token) {
         if (!inside(token)) return;
         const int v = static_cast<int>(token - v0);
@@ -245,8 +256,9 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
         else atomicAdd(&s_n[v], 1u);
         mark(s_touched, v);
       };
-      constexpr int kAhead = 8;
-      int64_t j0 = begin;
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) count(begin + e * kThreads + tid, early[e]);
+      int64_t j0 = begin + kAhead * kThreads;
       for (; j0 + kAhead * 4 * kThreads <= end + 1; j0 += kAhead * 4 * kThreads) {   // four tokens a load
         int32_t token[kAhead][4];
 #pragma unroll
@@ -267,35 +279,33 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
         for (int e = 0; e < kAhead; ++e)
           if (j0 + e * kThreads + tid <= end) count(j0 + e * kThreads + tid, token[e]);
       }
-      if (tid < r1 - 1 && inside(draft[tid])) {   // (k is below the threads)
-        mark(s_touched, static_cast<int>(draft[tid] - v0));
-        mark(s_drafted, static_cast<int>(draft[tid] - v0));
+      if (inside(drafted_token)) {
+        mark(s_touched, static_cast<int>(drafted_token - v0));
+        mark(s_drafted, static_cast<int>(drafted_token - v0));
       }
     }
     // The biases: of an id given more than once, the first place adds all of
     // them up, in their order.
-    constexpr int kBiases = SPECDEC_MAX_BIAS / kThreads;
-    for (int j = tid; j < p.n_bias; j += kThreads)
-      if (inside(ids[j])) atomicMin(&s_place[ids[j] - v0], static_cast<uint32_t>(j));
+#pragma unroll
+    for (int e = 0; e < kBiases; ++e)
+      if (inside(id[e])) atomicMin(&s_place[id[e] - v0], static_cast<uint32_t>(tid + e * kThreads));
     __syncthreads();
     if (p.n_bias > 0) {
       bool mine[kBiases];
 #pragma unroll
       for (int e = 0; e < kBiases; ++e) {
-        const int j = tid + e * kThreads;
-        const bool in = j < p.n_bias && inside(ids[j]);
-        mine[e] = in && s_place[ids[j] - v0] == static_cast<uint32_t>(j);
-        if (in && !mine[e]) s_again = 1;
+        mine[e] = inside(id[e]) && s_place[id[e] - v0] == static_cast<uint32_t>(tid + e * kThreads);
+        if (inside(id[e]) && !mine[e]) s_again = 1;
       }
       __syncthreads();
 #pragma unroll
       for (int e = 0; e < kBiases; ++e) {
         if (!mine[e]) continue;
-        const int j = tid + e * kThreads, v = static_cast<int>(ids[j] - v0);
-        float sum = bias[j];
+        const int v = static_cast<int>(id[e] - v0);
+        float sum = bias_of[e];
         if (s_again)
-          for (int y = j + 1; y < p.n_bias; ++y)
-            if (ids[y] == ids[j]) sum += bias[y];
+          for (int y = tid + e * kThreads + 1; y < p.n_bias; ++y)
+            if (ids[y] == id[e]) sum += bias[y];
         s_bias[v] = sum;
         mark(s_touched, v);
         mark(s_biased, v);
@@ -305,14 +315,24 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
   }
   // What the counts and biases do to the lane's logits: `held` bits say where the
   // repetition penalty applies, `add` is added.
-  const float rep = p.repetition ? p.repetition[i] : 1.f, less = 1.f / rep;
-  const float pres = p.presence ? p.presence[i] : 0.f, freq = p.frequency ? p.frequency[i] : 0.f;
+  const float less = 1.f / rep;
   uint32_t held[kUnits] = {}, drafted[kUnits] = {};
   float add[kUnits][8] = {};
   auto added = [&](uint32_t n, int v) {
     const float bias = s_biased[v >> 5] >> (v & 31) & 1u ? s_bias[v] : 0.f;
     const uint32_t told = n & ~kPrompt;
     return told ? bias - (freq * static_cast<float>(told) + pres) : bias;
+  };
+  // A drafted token's logit in slot r: its count grows from slot to slot.
+  auto changed = [&](float one, int v, int r) {
+    uint32_t n = s_n[v];
+    for (int j = 0; j < r; ++j)
+      if (load_invariant(draft + j) == static_cast<int32_t>(v0 + v)) {
+        if (end + 1 + j < answered) n |= kPrompt;
+        else ++n;
+      }
+    if (n) one *= one > 0.f ? less : rep;
+    return one + added(n, v);
   };
   if constexpr (kSparse) {
 #pragma unroll
@@ -351,27 +371,30 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
           }
           y = replaced<T>(y, z, touched[e]);
           for (uint32_t bits = drafted[e] & mask[e]; bits; bits &= bits - 1) {
-            const int b = __builtin_ctz(bits), v = at(e) + b;
-            uint32_t n = s_n[v];
-            for (int j = 0; j < r; ++j)
-              if (load_invariant(draft + j) == static_cast<int32_t>(v0 + v)) {
-                if (end + 1 + j < answered) n |= kPrompt;
-                else ++n;
-              }
-            float one = take<T>(now[e], b);
-            if (n) one *= one > 0.f ? less : rep;
-            y = give<T>(y, b, one + added(n, v));
+            const int b = __builtin_ctz(bits);
+            y = give<T>(y, b, changed(take<T>(now[e], b), at(e) + b, r));
           }
         }
       }
       if (mask[e] != 0xFFu) y = masked<T>(y, mask[e]);
-      store_unit(static_cast<T*>(p.out) + ((row0 + r) * p.V + v0) + at(e), y, size - at(e));
+      store_unit(static_cast<T*>(p.out) + ((row0 + r) * p.V + v0) + at(e), y);
     }
 #pragma unroll
     for (int e = 0; e < kUnits; ++e) {
       mask[e] = mask1[e];
       mask1[e] = mask2[e];
     }
+  }
+  // the vocabulary's last logits where it is no multiple of 8, a thread each
+  const int left = size - whole;
+  for (int j = tid; j < left * (r1 - r0); j += kThreads) {
+    const int r = r0 + j / left, v = whole + j % left;
+    const int64_t row = row0 + r;
+    T one = static_cast<const T*>(p.logits)[row * p.V + v0 + v];
+    if (kSparse && s_touched[v >> 5] >> (v & 31) & 1u)
+      one = static_cast<T>(changed(static_cast<float>(one), v, s_drafted[v >> 5] >> (v & 31) & 1u ? r : 0));
+    if (p.mask && !(p.mask[row * p.mask_stride + ((v0 + v) >> 5)] >> (v & 31) & 1u)) one = static_cast<T>(-__builtin_inff());
+    static_cast<T*>(p.out)[row * p.V + v0 + v] = one;
   }
 }
 
