@@ -149,6 +149,7 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
   __shared__ __align__(16) uint32_t s_n[kSparse ? kChunk : 4];
   __shared__ float s_bias[kSparse ? kChunk : 1];
   __shared__ uint32_t s_touched[kBitWords], s_drafted[kBitWords], s_biased[kBitWords];
+  __shared__ __align__(16) int32_t s_draft[SPECDEC_MAX_K];
   __shared__ int s_again;
   const LogitsLaunch& p = a.p;
   const int tid = threadIdx.x;
@@ -222,12 +223,12 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
     const float* bias = p.bias + static_cast<int64_t>(i) * p.n_bias;
     const int32_t* s = p.s + i * p.s_stride;
     int32_t early[kAhead], id[kBiases], drafted_token = -1;
-    float bias_of[kBiases];
+    float bias_at[kBiases];
 #pragma unroll
     for (int e = 0; e < kBiases; ++e) {
       const int j = tid + e * kThreads;
       id[e] = j < p.n_bias ? ids[j] : -1;
-      bias_of[e] = j < p.n_bias ? bias[j] : 0.f;
+      bias_at[e] = j < p.n_bias ? bias[j] : 0.f;
     }
     if (penal) {
 #pragma unroll
@@ -235,7 +236,7 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
         const int64_t j = begin + e * kThreads + tid;
         early[e] = j <= end ? s[j] : -1;
       }
-      if (tid < r1 - 1) drafted_token = draft[tid];   // (k is below the threads)
+      if (tid < r1 - 1) drafted_token = draft[tid];
     }
     uint32_t* s_place = reinterpret_cast<uint32_t*>(s_bias);
     auto inside = [&](int32_t token) { return token >= v0 && token < v0 + size; };
@@ -245,6 +246,7 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
 #pragma unroll
     for (int e = 0; e < kBiases; ++e)
       if (inside(id[e])) s_place[id[e] - v0] = ~0u;
+    if (tid < SPECDEC_MAX_K) s_draft[tid] = drafted_token;
     if (tid == 0) s_again = 0;
     __syncthreads();
     if (!kAtOnce && !in_place) read(r0, mask, x);
@@ -302,7 +304,7 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
       for (int e = 0; e < kBiases; ++e) {
         if (!mine[e]) continue;
         const int v = static_cast<int>(id[e] - v0);
-        float sum = bias_of[e];
+        float sum = bias_at[e];
         if (s_again)
           for (int y = tid + e * kThreads + 1; y < p.n_bias; ++y)
             if (ids[y] == id[e]) sum += bias[y];
@@ -318,22 +320,37 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
   const float less = 1.f / rep;
   uint32_t held[kUnits] = {}, drafted[kUnits] = {};
   float add[kUnits][8] = {};
-  auto added = [&](uint32_t n, int v) {
-    const float bias = s_biased[v >> 5] >> (v & 31) & 1u ? s_bias[v] : 0.f;
+  auto bias_of = [&](int v) { return s_biased[v >> 5] >> (v & 31) & 1u ? s_bias[v] : 0.f; };
+  auto added = [&](uint32_t n, float bias) {
     const uint32_t told = n & ~kPrompt;
     return told ? bias - (freq * static_cast<float>(told) + pres) : bias;
   };
-  // A drafted token's logit in slot r: its count grows from slot to slot.
-  auto changed = [&](float one, int v, int r) {
-    uint32_t n = s_n[v];
-    for (int j = 0; j < r; ++j)
-      if (load_invariant(draft + j) == static_cast<int32_t>(v0 + v)) {
-        if (end + 1 + j < answered) n |= kPrompt;
-        else ++n;
-      }
-    if (n) one *= one > 0.f ? less : rep;
-    return one + added(n, v);
+  // A drafted token's logit in slot r, whose count grows from slot to slot: bit
+  // j of `same` says that draft j is the token, bit j of `prompted` that it lies
+  // in the prompt.
+  auto drafts_like = [&](int v) {
+    uint64_t same = 0;
+    for (int j = 0; j < r1 - 1; j += 4) {
+      const int4 four = *reinterpret_cast<const int4*>(&s_draft[j]);
+      const int32_t token = static_cast<int32_t>(v0 + v);
+      same |= static_cast<uint64_t>((four.x == token ? 1u : 0u) | (four.y == token ? 2u : 0u) | (four.z == token ? 4u : 0u) |
+                                    (four.w == token ? 8u : 0u)) << j;
+    }
+    return same;
   };
+  auto before = [](int64_t j) { return j <= 0 ? 0 : j < 64 ? (uint64_t{1} << j) - 1 : ~uint64_t{0}; };
+  const uint64_t prompted = before(answered - end - 1);
+  auto changed = [&](float one, uint32_t n, uint64_t same, float bias, int r) {
+    const uint64_t seen = same & before(r);
+    n += __popcll(seen & ~prompted);
+    if (seen & prompted) n |= kPrompt;
+    if (n) one *= one > 0.f ? less : rep;
+    return one + added(n, bias);
+  };
+  // ... the first of a lane's unit, from registers: LDS would be waited for in every slot
+  uint64_t same[kUnits] = {};
+  uint32_t count_of[kUnits] = {};
+  float bias_first[kUnits] = {};
   if constexpr (kSparse) {
 #pragma unroll
     for (int e = 0; e < kUnits; ++e) {
@@ -344,7 +361,13 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
       for (int b = 0; b < 8; ++b) {
         const uint32_t n = s_n[at(e) + b];
         if (n) held[e] |= 1u << b;
-        add[e][b] = added(n, at(e) + b);
+        add[e][b] = added(n, bias_of(at(e) + b));
+      }
+      if (drafted[e]) {
+        const int v = at(e) + __builtin_ctz(drafted[e]);
+        same[e] = drafts_like(v);
+        count_of[e] = s_n[v];
+        bias_first[e] = bias_of(v);
       }
     }
   }
@@ -370,9 +393,13 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
             z[b] += add[e][b];
           }
           y = replaced<T>(y, z, touched[e]);
-          for (uint32_t bits = drafted[e] & mask[e]; bits; bits &= bits - 1) {
-            const int b = __builtin_ctz(bits);
-            y = give<T>(y, b, changed(take<T>(now[e], b), at(e) + b, r));
+          if (drafted[e]) {
+            const int b = __builtin_ctz(drafted[e]);
+            y = give<T>(y, b, changed(take<T>(now[e], b), count_of[e], same[e], bias_first[e], r));
+          }
+          for (uint32_t bits = drafted[e] & (drafted[e] - 1) & mask[e]; bits; bits &= bits - 1) {
+            const int b = __builtin_ctz(bits), v = at(e) + b;
+            y = give<T>(y, b, changed(take<T>(now[e], b), s_n[v], drafts_like(v), bias_of(v), r));
           }
         }
       }
@@ -392,7 +419,7 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
     const int64_t row = row0 + r;
     T one = static_cast<const T*>(p.logits)[row * p.V + v0 + v];
     if (kSparse && s_touched[v >> 5] >> (v & 31) & 1u)
-      one = static_cast<T>(changed(static_cast<float>(one), v, s_drafted[v >> 5] >> (v & 31) & 1u ? r : 0));
+      one = static_cast<T>(changed(static_cast<float>(one), s_n[v], drafts_like(v), bias_of(v), r));
     if (p.mask && !(p.mask[row * p.mask_stride + ((v0 + v) >> 5)] >> (v & 31) & 1u)) one = static_cast<T>(-__builtin_inff());
     static_cast<T*>(p.out)[row * p.V + v0 + v] = one;
   }
