@@ -628,6 +628,7 @@ __global__ __launch_bounds__(kThreads, DP > 128 && MT > 1 ? 1 : 2) void attend_k
 // the sums in turn.  Joined by the pair's last workgroup in the first kernel
 // instead, pairs of many pieces or queries took longer.
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, uint32_t lanes, uint32_t parts, uint32_t rows) {
+  constexpr int kAhead = 4;
   __shared__ f32x4 s_o[kThreads];
   __shared__ float s_m[kThreads], s_l[kThreads];
   const CacheView& c = a.c;
@@ -645,15 +646,39 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, uin
   f32x4 o = {};
   int bad = 0;
   if (live) {
-#pragma unroll 4
-    for (int s = part; s < pieces; s += parts) {
-      const int64_t piece = slot + s;
-      bad |= a.stat[piece * a.M].y == kBadPiece;
-      const float2 t = a.stat[piece * a.M + q];
-      const f32x4 v = *reinterpret_cast<const f32x4*>(a.part + (piece * a.M + q) * D + d);
-      const float top = __builtin_fmaxf(m, t.x), keep = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(t.x - top);
-      l = l * keep + t.y * f;
-      o = o * keep + v * f;
+    // kAhead pieces are read before the first is waited for; places behind the
+    // last stand for the first of these, with no weight
+    for (int s = part; s < pieces; s += parts * kAhead) {
+      float2 t[kAhead];
+      f32x4 v[kAhead];
+      float flag[kAhead];
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) {
+        const int at = s + e * static_cast<int>(parts);
+        const int64_t piece = slot + (at < pieces ? at : s);
+        flag[e] = a.stat[piece * a.M].y;
+        t[e] = a.stat[piece * a.M + q];
+        v[e] = *reinterpret_cast<const f32x4*>(a.part + (piece * a.M + q) * D + d);
+      }
+      float top = m;
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) {
+        if (s + e * static_cast<int>(parts) >= pieces) {
+          t[e] = float2{kLowest, 0.f};
+          v[e] = f32x4{};
+        }
+        bad |= flag[e] == kBadPiece;
+        top = __builtin_fmaxf(top, t[e].x);
+      }
+      const float keep = __builtin_amdgcn_exp2f(m - top);
+      l *= keep;
+      o *= keep;
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) {
+        const float f = __builtin_amdgcn_exp2f(t[e].x - top);
+        l += t[e].y * f;
+        o += v[e] * f;
+      }
       m = top;
     }
   }
