@@ -61,6 +61,7 @@ constexpr int kTile = 32;                 // entries a wave takes at a time
 constexpr int kMaxCutB = 1024;            // sequences that a workgroup scans
 constexpr uint32_t kLeastPiece = 4;       // tiles
 constexpr uint32_t kCus = 256;
+constexpr int kJoinAhead = 4;             // pieces that a group of lanes of the join reads at a time
 constexpr float kLowest = -3.0e38f;       // the maximum of no score
 constexpr float kSlack = 8.f;             // powers of two that a weight may exceed 1 by
 constexpr float kBadPiece = -1.f;         // a piece's sum of weights: it has met a page outside the pool
@@ -77,6 +78,7 @@ struct AttendArgs {
   uint32_t groups;        // of 16 * MT queries
   uint32_t items;         // workgroups a group
   uint32_t pieces;        // pieces that the batch's entries are cut into, about (0: pairs are not cut)
+  uint32_t joined;        // pieces of a pair that the join reads at a time
   float c2;               // scale * log2(e)
   uint32_t* dev_status;
 };
@@ -195,14 +197,19 @@ __device__ __forceinline__ uint32_t wave_last(uint32_t v) { return __builtin_amd
 
 // Finds the workgroup's piece by a scan of the sequences.  Pieces have at most
 // `most` tiles, a multiple of kLeastPiece; a sequence of more has as many equal
-// ones as that takes.
-// Unequal sequences of `t` tiles in all: most = t / a.pieces, rounded up, so
-// that there are at most a.pieces + pairs pieces, 2 * a.pieces of cut pairs.
+// ones as that takes.  The join takes as long as four tiles for every a.joined
+// pieces of a pair, so that a pair of `top` tiles is best cut into pieces of no
+// fewer than sqrt(4 * top / a.joined) (1521 to 30429 entries in three pairs of
+// one query: 14.0 us, 17.1 in pieces of four tiles).
+// Unequal sequences of `t` tiles in all: most = t / a.pieces, rounded up, or
+// that bound, so that there are at most a.pieces + pairs pieces, 2 * a.pieces
+// of cut pairs.
 // About equal ones: the pairs get as many pieces each as lets the CU with the
 // most of them end first, a piece counted as kLeastPiece tiles more than it has
-// for what it begins and ends with, and a.pieces pieces at most in all (35 x 2
-// KV heads of 256, window 5, 3762 to 4180 entries: 70 us, where about 256
-// pieces, four a pair, leave 24 CUs with a second one and take 96).
+// for what it begins and ends with, the join as above, and a.pieces pieces at
+// most in all (35 x 2 KV heads of 256, window 5, 3762 to 4180 entries: 70 us,
+// where about 256 pieces, four a pair, leave 24 CUs with a second one and take
+// 96).
 // False: no piece is left for this workgroup.
 __device__ __forceinline__ bool find_piece(const AttendArgs& a, uint32_t item, bool first, Piece* p) {
   constexpr int kEach = kMaxCutB / kThreads;
@@ -243,13 +250,15 @@ __device__ __forceinline__ bool find_piece(const AttendArgs& a, uint32_t item, b
     const uint32_t pairs = static_cast<uint32_t>(a.B * a.c.H), step = 1 + kCus / (64 * pairs), each = (lane + 1) * step;
     const uint32_t size = ((top + each - 1) / each + kLeastPiece - 1) / kLeastPiece * kLeastPiece;
     const uint32_t rounds = (pairs * each * a.groups + kCus - 1) / kCus;
-    const uint64_t time = static_cast<uint64_t>(rounds) * (size + kLeastPiece);
+    const uint64_t time = static_cast<uint64_t>(rounds) * (size + kLeastPiece) + 4 * each / a.joined;
     constexpr uint32_t kNever = (1u << 26) - 1;
     const uint32_t cost = (each == step || pairs * each <= a.pieces) && time < kNever ? static_cast<uint32_t>(time) : kNever;
     const uint32_t best = ~wave_last(wave_scan(~(cost << 6 | static_cast<uint32_t>(lane)), larger));
     most = __builtin_amdgcn_readlane(size, best & 63);
   } else {
-    most = (static_cast<uint32_t>((all + a.pieces - 1) / a.pieces) + kLeastPiece - 1) / kLeastPiece * kLeastPiece;
+    const uint32_t share = static_cast<uint32_t>((all + a.pieces - 1) / a.pieces);
+    const uint32_t least = static_cast<uint32_t>(__builtin_amdgcn_sqrtf(4.f * static_cast<float>(top) / static_cast<float>(a.joined)));
+    most = ((share > least ? share : least) + kLeastPiece - 1) / kLeastPiece * kLeastPiece;
   }
   uint32_t mine[kEach], pieces = 0, cut = 0, at[kEach], cut_at[kEach];
 #pragma unroll
@@ -628,7 +637,7 @@ __global__ __launch_bounds__(kThreads, DP > 128 && MT > 1 ? 1 : 2) void attend_k
 // the sums in turn.  Joined by the pair's last workgroup in the first kernel
 // instead, pairs of many pieces or queries took longer.
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, uint32_t lanes, uint32_t parts, uint32_t rows) {
-  constexpr int kAhead = 4;
+  constexpr int kAhead = kJoinAhead;
   __shared__ f32x4 s_o[kThreads];
   __shared__ float s_m[kThreads], s_l[kThreads];
   const CacheView& c = a.c;
@@ -774,6 +783,12 @@ hipError_t launch_attend(const AttendLaunch& p, hipStream_t stream) {
   a.part = reinterpret_cast<float*>(static_cast<char*>(p.workspace) + (8 * static_cast<int64_t>(p.B) + 255) / 256 * 256);
   a.stat = reinterpret_cast<float2*>(a.part + plan.slots * a.M * c.D);
   const bool paged = c.table && c.cap < c.width;
+  // few queries: a workgroup each, so that many pieces are read at a time; many: several a workgroup
+  uint32_t lanes = 1;
+  while (lanes * 4 < static_cast<uint32_t>(c.D)) lanes *= 2;
+  const int64_t pairs = static_cast<int64_t>(p.B) * c.H;
+  const uint32_t slots = kThreads / lanes, parts = pairs * a.M <= 2048 ? slots : 1, rows = slots / parts;
+  a.joined = parts * kJoinAhead;
   const int64_t blocks = (plan.items + 7) / 8 * 8 * plan.groups;
   if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
   const hipError_t e = launch_blocks(blocks, kThreads, [&](int64_t at, uint32_t count) {
@@ -792,11 +807,6 @@ hipError_t launch_attend(const AttendLaunch& p, hipStream_t stream) {
     }
   });
   if (e != hipSuccess || !plan.pieces) return e;
-  // few queries: a workgroup each, so that many pieces are read at a time; many: several a workgroup
-  uint32_t lanes = 1;
-  while (lanes * 4 < static_cast<uint32_t>(c.D)) lanes *= 2;
-  const int64_t pairs = static_cast<int64_t>(p.B) * c.H;
-  const uint32_t slots = kThreads / lanes, parts = pairs * a.M <= 2048 ? slots : 1, rows = slots / parts;
   return launch_blocks(pairs * ((a.M + rows - 1) / rows), kThreads, [&](int64_t at, uint32_t count) {
     a.base = static_cast<uint32_t>(at);
     attend_join_kernel<<<count, kThreads, 0, stream>>>(a, lanes, parts, rows);
