@@ -15,7 +15,7 @@
 // 2^24 an fp32 product would be off by up to half a radian.
 //
 // Bounds and figures.  Few tokens: the waits in turn for length, page and row;
-// 4.5 us for one token of 32 + 16 heads of 128 on pages, 5.0 us for 48 tokens
+// 4.5 us for one token of 32 + 16 heads of 128 on pages, 4.9 us for 48 tokens
 // of 32 + 64 heads (a call takes 5.4 either way).  Many: bytes; 64 windows of
 // 33 tokens, 28 + 8 heads of 128 in fp32, 58 MB, 13.1 us, 4.5 TB/s, the rate
 // of a large copy.  With a workgroup a few heads of any token and the angles in

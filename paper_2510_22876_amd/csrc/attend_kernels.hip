@@ -41,12 +41,12 @@
 //
 // Figures (us of both kernels, and TB/s of the bytes that must be read and
 // written; plain reads reach 6.2).  One query of 32 + 8 heads over 1000
-// entries, 16 a page: 7.2 + 4.0.  Whole pairs, 8 windows of 6, 32 + 32 heads,
+// entries, 16 a page: 7.4 + 4.3.  Whole pairs, 8 windows of 6, 32 + 32 heads,
 // 128 to 1024 entries: 15.4 and 3.9; its longest pair is 527 KB, of which a
 // workgroup reads 50 KB a us.  Cut, 32 windows of 8, 32 + 8 heads, 64 to 4096
-// entries, 64 a page: 40.0 + 5.2 and 3.7; 64 windows of 5, 28 + 4 heads, 512 to
-// 8192 entries: 81.0 + 5.5 and 4.3; one window of 6 over 150001 entries: 108.0
-// + 5.7 and 5.4.  The matrix products of these three would take 4.5, 11.5 and
+// entries, 64 a page: 39.9 + 4.9 and 3.7; 64 windows of 5, 28 + 4 heads, 512 to
+// 8192 entries: 81.1 + 5.4 and 4.3; one window of 6 over 150001 entries: 108.4
+// + 4.9 and 5.4.  The matrix products of these three would take 4.5, 11.5 and
 // 13 us: what is left is uneven pieces, their starts and ends, and the second
 // launch.
 #include "forward_common.h"
@@ -633,7 +633,7 @@ __global__ __launch_bounds__(kThreads, DP > 128 && MT > 1 ? 1 : 2) void attend_k
 
 // Joins the pieces of a pair.  `parts` groups of `lanes` lanes take a query's
 // pieces in turn and are summed in their order; a workgroup takes `rows`
-// queries.  3 to 6 us: a launch, and the waits for the plan, the statistics and
+// queries.  3 to 5 us: a launch, and the waits for the plan, the statistics and
 // the sums in turn.  Joined by the pair's last workgroup in the first kernel
 // instead, pairs of many pieces or queries took longer.
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, uint32_t lanes, uint32_t parts, uint32_t rows) {

@@ -19,8 +19,8 @@
 // computed again from the counts.
 //
 // Figures.  32 windows of 8, 128256 logits in bf16, all penalties, 64 biases, a
-// mask that allows nine tenths, histories of 64 to 4096: 32.3 us for 136 MB,
-// 4.2 TB/s; a plain copy of the logits takes 25.9, and so does this kernel with
+// mask that allows nine tenths, histories of 64 to 4096: 32.7 us for 136 MB,
+// 4.1 TB/s; a plain copy of the logits takes 25.9, and so does this kernel with
 // nothing to change, 27.3 with the mask.  In place with a mask that allows a
 // twentieth, 64 windows of 5, 151936 logits: 34.1 us; four fifths of the
 // 64-byte lines hold an allowed logit and are read.  1000 logits, or one row of 128256: 5 to 6
