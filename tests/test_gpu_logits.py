@@ -113,6 +113,21 @@ def test_matches_64_bits(sd, name, unpadded):
     assert torch.equal(out.float().nan_to_num(7.0), again.float().nan_to_num(7.0)), "in place differs"
 
 
+@pytest.mark.parametrize("V", [5, 8, 21, 2051])
+def test_many_drafts_a_unit(sd, V):
+    """Drafts of a small vocabulary: several and repeated ones among eight neighbouring logits and among the last few, with
+    prompts that end before, among and behind them."""
+    c = _case(4, 64, V, "bf16", [7, 30, 1, 12], 6, n_bias=4)
+    r = np.random.default_rng(8)
+    c["draft"] = (V - 1 - r.integers(0, min(V, 20), size=(4, 64))).astype(np.int32)
+    c["prompt"] = np.asarray([3, 40, 70, 200], np.int32)
+    out, status = _run(sd, c)
+    assert status == 0
+    _check(c, out)
+    again, _ = _run(sd, c, in_place=True)
+    assert torch.equal(out.view(torch.int16), again.view(torch.int16)), "in place differs"
+
+
 @pytest.mark.parametrize("which", range(3))
 def test_each_penalty_alone(sd, which):
     c = _case(2, 3, 3000, "f32", [30, 400], 2)
