@@ -371,7 +371,8 @@ __global__ __launch_bounds__(kThreads, DP > 128 && MT > 1 ? 1 : 2) void attend_k
   const __bf16 *kp = static_cast<const __bf16*>(c.k) + head, *vp = static_cast<const __bf16*>(c.v) + head;
   if constexpr (!kPaged) {
     const int64_t first = first_entry(c, i, n, a.T);
-    bad = first < 0;
+    bad = first < 0;   // no entry is read then
+    if (bad) c1 = c0;
     kp += first;
     vp += first;
   }

@@ -340,3 +340,23 @@ def test_offsets_past_32_bits(sd):
     want, bound = ref.attend(q[2], e[0].double()[:, None], e[1].double()[:, None], n, D ** -0.5)
     ref.check(out[2], want, bound, "the far row")
     assert bool((out[:2] == 0).all())
+
+
+@pytest.mark.parametrize("G", [1, 12])
+@pytest.mark.parametrize("n", [[60, 30, 0, 62, 45], [9000, 20, 400, 8000, 7000]])
+def test_slots_outside_a_pool_of_whole_sequences(sd, n, G):
+    """One page a sequence: a slot outside the pool is flagged and its sequence left untouched before anything is read
+    from there, whole and cut, also on the first layer, where nothing lies before the pool."""
+    T, H, D = 3, 2, 64
+    c = ref.Cache(n, T, H, D, page=max(n) + T + 1, layers=1, layer=0, room=0, slots=True)
+    c.fill(T, torch.Generator().manual_seed(1))
+    q = _queries(c, G * H, 5)
+    assert c.table_np.shape == (5, 1) and c.shape[2] == 5
+    table = c.table_np.copy()
+    table[0], table[2], table[3] = -1, c.shape[2], 2 ** 31 - 1
+    out, status = _run(sd, c, q, table=torch.as_tensor(table, device="cuda"))
+    assert status == sd.DEV_BAD_SLOT
+    _check(c, q, out, skip=(0, 2, 3))
+    out, status = _run(sd, c, q)
+    assert status == 0
+    _check(c, q, out)
