@@ -654,7 +654,10 @@ specdec_status_t specdec_append_paged(const void* qkv, int32_t dtype, int32_t B,
  *   workspace specdec_attend_workspace_bytes(B, T, Hq, H, D, max_len) bytes,
  *             16-byte aligned, with max_len = W_in for the batch; it needs no
  *             initialisation and keeps nothing between calls.  Calls that may
- *             run at the same time need one each.
+ *             run at the same time need one each.  The bytes never fall as B, T
+ *             or max_len grows: with the same heads, a workspace for the most
+ *             sequences, queries and entries serves every smaller call.  Up to
+ *             26 MB for heads of at most 128 and 512 queries a KV head.
  * Scores, the softmax's statistics and the sums are fp32; the weights p are
  * rounded to bf16 for the matrix cores, and their sum is taken of the rounded
  * ones.  The result does not depend on the order in which workgroups run.

@@ -720,13 +720,17 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, uin
 // How a call is divided: tiles of 16 queries a workgroup and groups of them,
 // workgroups a group, and the pieces that the batch's entries are cut into
 // (0: pairs are not cut).
+constexpr int64_t kLeastCut = 320 * 1024;        // bytes of the shortest pair that is cut
+constexpr int64_t kMostPieces = 2 * kCus, kFewestPieces = 8;   // kMostPieces over the groups, and no fewer than these
+int64_t most_tiles(int64_t D) { return D > 128 ? 2 : 3; }
+int64_t pair_bytes(int64_t D, int64_t max_len) { return max_len * (D > 128 ? D : 128) * 4; }
 struct Plan {
   int tiles;
   int64_t groups, items, pieces, slots;
 };
 Plan plan_of(int64_t B, int64_t T, int64_t Hq, int64_t H, int64_t D, int64_t max_len) {
   Plan p;
-  const int64_t tiles = (T * (Hq / H) + 15) / 16, most = D > 128 ? 2 : 3, pairs = B * H;
+  const int64_t tiles = (T * (Hq / H) + 15) / 16, most = most_tiles(D), pairs = B * H;
   p.groups = (tiles + most - 1) / most;
   p.tiles = static_cast<int>((tiles + p.groups - 1) / p.groups);
   // A workgroup reads about 50 KB a microsecond (smaller heads than 128 do not
@@ -735,12 +739,11 @@ Plan plan_of(int64_t B, int64_t T, int64_t Hq, int64_t H, int64_t D, int64_t max
   // with other pairs a longer one may stay whole (Vicuna-7B's batch of 8, 256
   // pairs of at most 1030 entries: 16.1 us whole, 19.5 cut; 8 pairs of 1001:
   // 13.7 and 11.6).
-  const int64_t bytes = max_len * (D > 128 ? D : 128) * 4;
-  const bool cut = bytes > (pairs >= kCus / 2 ? 768 : 320) * 1024 && B <= kMaxCutB && pairs <= 4096;
+  const bool cut = pair_bytes(D, max_len) > (pairs >= kCus / 2 ? 768 * 1024 : kLeastCut) && B <= kMaxCutB && pairs <= 4096;
   // Pieces of unequal sequences: 3/2 a CU (64 of 512 to 8192, 256 pairs: 104 us
   // with 1, 91 with 3/2, 98 with 2), more where few pairs add their number.
-  const int64_t wanted = pairs > kCus / 2 ? kCus * 3 / 2 : kCus * 2;
-  p.pieces = !cut ? 0 : p.groups >= wanted / 8 ? 8 : wanted / p.groups;
+  const int64_t wanted = pairs > kCus / 2 ? kMostPieces * 3 / 4 : kMostPieces;
+  p.pieces = !cut ? 0 : p.groups >= wanted / kFewestPieces ? kFewestPieces : wanted / p.groups;
   p.items = pairs + p.pieces;
   p.slots = 2 * p.pieces;
   return p;
@@ -758,9 +761,15 @@ void launch_tiles(const AttendArgs& a, bool paged, uint32_t blocks, hipStream_t 
 
 }  // namespace
 
+// Enough for the call and, with the same heads, for every one of fewer
+// sequences, queries or entries, though these may be cut into more pieces: of
+// the slots' 2 * pieces * M rows (M queries a pair), pieces * M is at most
+// kFewestPieces * M, or kMostPieces times the queries that a workgroup takes.
 int64_t attend_workspace(int64_t B, int64_t T, int64_t Hq, int64_t H, int64_t D, int64_t max_len) {
-  const Plan p = plan_of(B, T, Hq, H, D, max_len);
-  return (8 * B + 255) / 256 * 256 + p.slots * T * (Hq / H) * (D * 4 + 8) + 256;
+  const int64_t M = T * (Hq / H), once = 16 * most_tiles(D);
+  const int64_t spread = kMostPieces * (M < once ? M : once), fewest = kFewestPieces * M;
+  const int64_t rows = pair_bytes(D, max_len) > kLeastCut ? 2 * (spread > fewest ? spread : fewest) : 0;
+  return (8 * B + 255) / 256 * 256 + rows * (D * 4 + 8) + 256;
 }
 
 hipError_t launch_attend(const AttendLaunch& p, hipStream_t stream) {

@@ -727,7 +727,8 @@ def attend_workspace_bytes(B: int, T: int, Hq: int, H: int, D: int, max_len: int
 
 def alloc_attend_workspace(B: int, T: int, Hq: int, H: int, D: int, max_len: int, device="cuda") -> torch.Tensor:
     """A workspace tensor for specdec_attend_window (max_len = W_in) and
-    specdec_attend_paged (needs no initialisation)."""
+    specdec_attend_paged (needs no initialisation); it also serves calls of
+    fewer sequences, queries and entries."""
     n = attend_workspace_bytes(B, T, Hq, H, D, max_len)
     return torch.empty((n + 15) // 16 * 2, dtype=torch.int64, device=device)
 

@@ -151,3 +151,22 @@ def test_wrappers_refuse_host_tensors(sd):
         sd.specdec_attend_paged(q, kv, 0, i32[None], i32, 4, q.clone(), i32)
     with pytest.raises(ValueError):
         sd.specdec_process_logits(torch.zeros((1, 1, 5)), torch.zeros((1, 1, 5)))
+
+
+def test_attend_workspace_serves_smaller_calls(sd):
+    """The bytes never fall as a batch, a window or a length grows: one workspace lasts a whole run, though a smaller
+    batch may be cut into more pieces than a larger one."""
+    f = sd.attend_workspace_bytes
+    lens = [65, 300, 640, 641, 1030, 1536, 1537, 8192, 1 << 24]
+    for Hq, H, D in [(32, 32, 128), (32, 8, 128), (28, 4, 128), (4, 1, 128), (4, 2, 16), (12, 12, 80), (8, 2, 256), (96, 1, 200)]:
+        for T in (1, 5, 12, 13, 65):
+            for most in lens:
+                sizes = [f(B, T, Hq, H, D, most) for B in (1, 2, 3, 8, 16, 17, 32, 33, 64, 128, 129, 512, 1024, 1025, 4097)]
+                assert sizes == sorted(sizes) and sizes[0] > 0, (Hq, H, D, T, most)
+        for B in (1, 8, 33, 64, 1025):
+            for most in lens:
+                sizes = [f(B, T, Hq, H, D, most) for T in range(1, 66)]
+                assert sizes == sorted(sizes), (Hq, H, D, B, most)
+            for T in (1, 6, 65):
+                sizes = [f(B, T, Hq, H, D, most) for most in lens]
+                assert sizes == sorted(sizes), (Hq, H, D, B, T)

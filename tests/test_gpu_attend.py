@@ -360,3 +360,24 @@ def test_slots_outside_a_pool_of_whole_sequences(sd, n, G):
     out, status = _run(sd, c, q)
     assert status == 0
     _check(c, q, out)
+
+
+def test_one_workspace_for_a_shrinking_batch(sd):
+    """A workspace of the whole batch, whose pairs stay whole, serves every smaller batch, whose pairs are cut, shorter
+    windows and other widths; nothing beyond its bytes is written."""
+    Hq, H, D, n = 32, 32, 128, [990, 700, 10, 990, 5, 64, 128, 33]
+    nb = sd.attend_workspace_bytes(len(n), 6, Hq, H, D, 1500)
+    space = torch.full((nb + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    for B, T, width in ((8, 6, 1500), (3, 6, 1100), (1, 5, 996), (2, 1, 1500), (4, 3, 993)):
+        c = ref.Cache(n[:B], T, H, D, layers=1, layer=0, width=width)
+        c.fill(T, torch.Generator().manual_seed(B))
+        q = _queries(c, Hq, B)
+        out = torch.full(q.shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+        sd.specdec_attend_window(q.cuda(), c.kv.cuda(), 0, c.W_in, c.pad, out, space[:nb])
+        torch.cuda.synchronize()
+        assert bool((space[nb:] == 0x5A).all())
+        for i in {0, B - 1}:
+            k, v = c.entries(i, n[i] + T)
+            for h in (0, Hq - 1):
+                want, bound = ref.attend(q[i][:, h:h + 1], k[:, h:h + 1], v[:, h:h + 1], n[i], D ** -0.5)
+                ref.check(out[i][:, h:h + 1].cpu(), want, bound, f"row {i} of {B}, head {h}")
