@@ -104,9 +104,10 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   const int64_t entry = c.table ? page * c.row_stride + static_cast<int64_t>(static_cast<uint32_t>(n + r) % P) * D
                                 : i * c.row_stride + (static_cast<int64_t>(c.width) - p.T + r) * D;
   __syncthreads();
-  // x = x * cs + partner * sn; elements that are not rotated have 1 and 0
+  // x = x * cs + partner * sn for the lane's first `turned` elements; the others
+  // stay as they are, and no infinity or NaN among them reaches another
   float cs[8], sn[8];
-  bool turns = false;   // any of the lane's
+  const int beyond = 2 * p.half - d0, turned = beyond < 0 ? 0 : beyond;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int d = d0 + e;
@@ -117,7 +118,6 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
       const int j = p.adjacent ? d >> 1 : second ? d - p.half : d;
       cs[e] = s_cos[j];
       sn[e] = second ? s_sin[j] : -s_sin[j];
-      turns = true;
     }
   }
   float* row = s_row + group * a.lanes * 8;
@@ -143,8 +143,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
           const float y = x[e], z = x[e + 1];
-          x[e] = y * cs[e] + z * sn[e];
-          x[e + 1] = z * cs[e + 1] + y * sn[e + 1];
+          x[e] = e < turned ? y * cs[e] + z * sn[e] : y;
+          x[e + 1] = e < turned ? z * cs[e + 1] + y * sn[e + 1] : z;
         }
       }
     } else if (p.half > 0) {
@@ -154,11 +154,11 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
         *reinterpret_cast<f32x4*>(row + d0 + 4) = f32x4{x[4], x[5], x[6], x[7]};
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      if (live && turns && (query || key)) {
+      if (live && turned > 0 && (query || key)) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int d = d0 + e, other = d >= 2 * p.half ? d : d < p.half ? d + p.half : d - p.half;
-          x[e] = x[e] * cs[e] + row[other] * sn[e];
+          x[e] = e < turned ? x[e] * cs[e] + row[other] * sn[e] : x[e];
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

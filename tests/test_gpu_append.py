@@ -150,3 +150,29 @@ def test_split_over_launches(sd, monkeypatch):
     monkeypatch.setenv("SPECDEC_MAX_LAUNCH_ITEMS", str(256 * 5))
     parts = _run(sd, c, x, w, f, False)
     assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(whole[:2], parts[:2]))
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("D, half, adjacent", [(16, 4, True), (16, 5, True), (16, 0, True), (16, 5, False), (16, 4, False), (24, 7, False),
+                                               (128, 33, False), (256, 66, True)])
+def test_unrotated_elements_stay_as_they_are(sd, dtype, D, half, adjacent):
+    """Infinities, NaN and -0.0 beyond the rotated elements, of which a lane may hold both kinds, are copied and reach no
+    other element."""
+    c = ref.Cache([3, 70], 2, 2, D)
+    c.fill(0, torch.Generator().manual_seed(1))
+    x, w, f = _inputs(c, 4, DT[dtype], half, False, 7)
+    odd = torch.tensor([float("inf"), float("-inf"), float("nan"), -0.0], dtype=DT[dtype])
+    for h in range(6):                                    # queries and keys
+        for j, d in enumerate(range(2 * half + h % 2, D, 2 if adjacent else 3)):
+            x[:, :, h, d] = odd[(j + h) % 4]
+    q, kv, status = _run(sd, c, x, w, f, adjacent)
+    assert status == 0
+    _check(c, x, w, f, adjacent, q, kv)
+    plain = x.to(torch.float32).to(torch.bfloat16)
+    same = lambda a, b: torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(   # noqa: E731
+        a[~torch.isnan(a)].view(torch.int16), b[~torch.isnan(b)].view(torch.int16))
+    assert same(q[..., 2 * half:], plain[:, :, :4, 2 * half:])
+    for i, n in enumerate(c.n):
+        for r in range(c.T):
+            row, col = c.where(i, n + r)
+            assert same(kv[c.layer, 0, row, :, col, 2 * half:], plain[i, r, 4:6, 2 * half:])
