@@ -324,11 +324,12 @@ __global__ __launch_bounds__(kThreads) void logits_kernel(LogitsArgs a) {
     }
   }
   // What the counts and biases do to the lane's logits: `held` bits say where the
-  // repetition penalty applies, `add` is added.
+  // repetition penalty applies, `add` is added; -0.0 where nothing is, which
+  // changes no value, and no -0.0 to 0.0.
   const float less = 1.f / rep;
   uint32_t held[kUnits] = {}, drafted[kUnits] = {};
   float add[kUnits][8] = {};
-  auto bias_of = [&](int v) { return s_biased[v >> 5] >> (v & 31) & 1u ? s_bias[v] : 0.f; };
+  auto bias_of = [&](int v) { return s_biased[v >> 5] >> (v & 31) & 1u ? s_bias[v] : -0.f; };
   auto added = [&](uint32_t n, float bias) {
     const uint32_t told = n & ~kPrompt;
     return told ? bias - (freq * static_cast<float>(told) + pres) : bias;

@@ -219,3 +219,32 @@ def test_offsets_past_32_bits(sd):
     sd.specdec_process_logits(x, x, s, 2, draft=torch.empty((B, 0), dtype=torch.int32, device="cuda"), frequency=f)
     torch.cuda.synchronize()
     assert bool((x[:, 0, V - 1] == -6).all()) and int((x != 0).sum()) == B
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("V", [21, 4096, 5001])
+def test_untouched_logits_keep_their_bits(sd, dtype, V):
+    """-0.0 among them: a drafted token's logit ahead of its draft, a prompt's under a penalty of answered tokens alone, and
+    logits that only share a unit of eight with changed ones."""
+    c = _case(1, 3, V, dtype, [40], 9, n_bias=2)
+    c["s"][:] = 1
+    c["s"][0, 5] = V - 2
+    c["draft"] = np.asarray([[3, V - 1, 3]], np.int32)
+    c["prompt"] = np.asarray([30], np.int32)
+    c["bias_ids"] = np.asarray([[6, 6]], np.int32)
+    c["pen"] = [None, c["pen"][1], c["pen"][2]]
+    x = c["logits"]
+    x[0, :, :10] = -0.0
+    x[0, :, -4:] = -0.0
+    changed = torch.zeros_like(x, dtype=torch.bool)
+    changed[0, :, [1, 6]] = True                          # the history and the bias
+    changed[0, 1:, 3] = True
+    changed[0, 2:, V - 1] = True
+    out, status = _run(sd, c)
+    assert status == 0
+    _check(c, out)
+    whole = torch.int32 if dtype == "f32" else torch.int16
+    assert torch.equal(out.view(whole)[~changed], x.view(whole)[~changed])
+    assert not bool((out.view(whole)[changed] == x.view(whole)[changed]).any())
+    again, _ = _run(sd, c, in_place=True)
+    assert torch.equal(out.view(whole), again.view(whole)), "in place differs"
