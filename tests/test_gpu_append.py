@@ -176,3 +176,18 @@ def test_unrotated_elements_stay_as_they_are(sd, dtype, D, half, adjacent):
         for r in range(c.T):
             row, col = c.where(i, n + r)
             assert same(kv[c.layer, 0, row, :, col, 2 * half:], plain[i, r, 4:6, 2 * half:])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-5])
+def test_norms_of_tiny_and_huge_heads(sd, dtype, eps):
+    """Squares that fp32 does not hold: their mean below its normal numbers, or beyond its largest."""
+    c = ref.Cache([4, 9], 2, 2, 96)
+    c.fill(0, torch.Generator().manual_seed(1))
+    x, w, f = _inputs(c, 4, torch.float32, 16, True, 11)
+    size = 2.0 ** torch.tensor([-120.0, -70.0, -64.0, 62.0, 100.0, 0.0])   # queries and keys; the last is ordinary
+    x[:, :, :6] *= size[:, None]
+    x, w = x.to(DT[dtype]), [t.to(DT[dtype]) for t in w]
+    q, kv, status = _run(sd, c, x, w, f, False, eps=eps)
+    assert status == 0
+    _check(c, x, w, f, False, q, kv, eps=eps)
