@@ -497,6 +497,7 @@ struct Attend {
     q = dense<void>(q_, at::kBFloat16, {B, T, Hq, kv.D});
     out = dense<void>(out_, at::kBFloat16, {B, T, Hq, kv.D});
     ws = workspace(ws_, lib.attend_workspace_bytes(B, T, Hq, kv.H, kv.D, max_len));
+    need(tensor(ws_).is_contiguous());   // its bytes are then its own
     if (scale_ == Py_None) {
       scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(kv.D)));
     } else {

@@ -748,6 +748,8 @@ def _check_attend(q, kv, out, workspace, max_len, dev_status):
     nb = workspace.numel() * workspace.element_size()
     if nb < attend_workspace_bytes(B, T, Hq, d.H, D, max_len) or not workspace.is_cuda:
         raise ValueError("workspace too small")
+    if not workspace.is_contiguous():   # a view of fewer bytes than its elements count
+        raise ValueError("workspace must be contiguous")
     return B, T, Hq, d, nb
 
 

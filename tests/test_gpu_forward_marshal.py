@@ -99,3 +99,17 @@ def test_refused_arguments_raise_alike(sd, monkeypatch, page):
                 said.append((e.type, str(e.value)))
             assert said[0] == said[1], (name, change)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("page", [0, 8])
+def test_workspace_views_with_gaps_or_repeats_are_refused(sd, monkeypatch, page):
+    """Their elements count more or other bytes than are theirs to write."""
+    native = sd._native
+    f, args, _ = _calls(sd, page)["attend"]
+    ws = args["workspace"]
+    for view in (ws[:1].expand(ws.numel()), torch.empty((ws.numel(), 2), dtype=ws.dtype, device="cuda")[:, 0]):
+        for route in (native, None):
+            monkeypatch.setattr(sd, "_native", route)
+            with pytest.raises(ValueError, match="contiguous"):
+                f(**{**args, "workspace": view})
+    torch.cuda.synchronize()
