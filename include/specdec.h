@@ -709,8 +709,10 @@ specdec_status_t specdec_attend_paged(const void* q, int32_t B, int32_t T, int32
  * begin and lens.  A slot whose mask allows no token becomes
  * -inf throughout and is flagged SPECDEC_DEV_EMPTY_MASK: greedy verification
  * then answers token 0, stochastic verification an unspecified one.
- * The arithmetic is fp32 with one rounding to `dtype` at the end; a logit that
- * none of these changes is copied as it is.  Limits as specdec_verify_greedy.
+ * The arithmetic is fp32 with one rounding to `dtype` at the end: a product
+ * with 1 / repetition, and one addend, the sum of the biases less what
+ * frequency and presence take off.  A logit that none of these changes is
+ * copied as it is.  Limits as specdec_verify_greedy.
  */
 specdec_status_t specdec_process_logits(const void* logits, void* out, int32_t dtype, int32_t B, int32_t k, int32_t V,
                                         const int32_t* s, int64_t s_stride, int32_t width, const int32_t* draft,

@@ -15,11 +15,11 @@
 // 2^24 an fp32 product would be off by up to half a radian.
 //
 // Bounds and figures.  Few tokens: the waits in turn for length, page and row;
-// 4.5 us for one token of 32 + 16 heads of 128 on pages, 4.9 us for 48 tokens
+// 4.6 us for one token of 32 + 16 heads of 128 on pages, 5.0 us for 48 tokens
 // of 32 + 64 heads (a call takes 5.4 either way).  Many: bytes; 64 windows of
-// 33 tokens, 28 + 8 heads of 128 in fp32, 58 MB, 13.1 us, 4.5 TB/s, the rate
-// of a large copy.  With a workgroup a few heads of any token and the angles in
-// LDS the last took 22.8 us.
+// 33 tokens, 28 + 8 heads of 128 in fp32, 58 MB, 13.3 to 13.4 us a call among
+// others, 4.4 TB/s, the rate of a large copy (12.8 to 15.9 under the profiler).
+// With a workgroup a few heads of any token and the angles in LDS it took 22.8.
 #include "forward_common.h"
 
 #include <type_traits>
